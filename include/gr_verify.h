@@ -16,11 +16,17 @@
  *              inverse-CDF draw from it (App. A, multi-draft procedure, step 3).
  *   gr_solve_verify, gr_solve_logits_verify  the two steps in one call.
  *
+ * and what a decoder does beside them, on the same rows and paths:
+ *   gr_draft, gr_draft_logits  the n i.i.d. drafts of every row (App. A, multi-draft procedure, step 1).
+ *   gr_beam_select             the best continuations of the beams of a sequence.
+ *   gr_beam_reorder            the states (attention caches, recurrent states) of beams or paths follow their parents.
+ *   gr_page_update             block tables, slot maps and the free list of a paged cache after lengths have changed.
+ *
  * Conventions
  *   - every pointer argument except `out`, `cfg` and host-side scalars is a DEVICE pointer
  *     owned by the caller; the library never frees or keeps them beyond what is stated;
  *   - all work is enqueued on `hip_stream` (a hipStream_t passed as void*; NULL = the
- *     default stream); gr_solve, gr_accept_sweep, gr_verify and the inspection calls neither
+ *     default stream); gr_solve, gr_accept_sweep, gr_verify, the calls beside the verification and the inspection calls neither
  *     allocate nor synchronise with the host (gr_create / gr_destroy allocate and free, and
  *     gr_profile_read waits for its events);
  *   - return value 0 = success, negative = call-level error (see GR_E*).  Argument and state errors
@@ -46,7 +52,8 @@ typedef struct gr_handle_s* gr_handle;
 #define GR_ENOMEM       (-2)   /* device allocation failed */
 #define GR_ESTATE       (-3)   /* gr_verify / gr_policy_* before a successful gr_solve */
 #define GR_EHIP         (-4)   /* a HIP runtime call failed */
-#define GR_EUNSUPPORTED (-5)   /* V >= 2^24 with a support above GR_MAX_SUPPORT; dense export of such a policy */
+#define GR_EUNSUPPORTED (-5)   /* V >= 2^24 with a support above GR_MAX_SUPPORT; dense export of such a policy; drafts from a top-k
+                                  above GR_MAX_SUPPORT; a nucleus cut of rows given as logits */
 #define GR_ECAPACITY    (-6)   /* more rows than the fixed scratch of gr_accept_sweep_noalloc holds */
 
 /* per-row status written by gr_solve */
@@ -54,10 +61,18 @@ typedef struct gr_handle_s* gr_handle;
 #define GR_ROW_TRUNC_CAP  1    /* a program needed more than max_T variables (App. "Truncated Solver Details") */
 #define GR_ROW_ITER_CAP   2    /* iteration cap reached before the gradient criterion (same appendix) */
 #define GR_ROW_BAD        3    /* NaN / negative entry, or a row sum further than 1e-3 from 1 */
+#define GR_ROW_NO_ROOM    4    /* gr_page_update: too few free blocks, or slots, for this request and those before it */
 
 #define GR_MAX_SUPPORT  256    /* largest top-k support (|V_0|) the LDS-resident path holds */
 #define GR_MAX_T        128    /* largest number of variables of one convex program */
 #define GR_MAX_N         16    /* largest number of drafts */
+#define GR_MAX_BEAMS     64    /* largest number of beams of a sequence, and of continuations chosen */
+#define GR_MAX_REQUESTS 8192   /* largest number of requests of gr_page_update */
+
+/* element types of logits */
+#define GR_F32  0
+#define GR_BF16 1
+#define GR_F16  2
 
 typedef struct {
     int    max_iter;   /* cap on the evaluations of the routed masses of ONE convex program (App. "Truncated Solver
@@ -203,6 +218,99 @@ int gr_solve_logits_verify(gr_handle h, const float* target_logits, const float*
                            const float* draft_temperature, int n, int k, float tol, int B, int V,
                            const int* drafts, const float* uniforms, float* accept_prob, int* status,
                            int* token, unsigned char* accepted, void* hip_stream);
+
+/* What a decoder does beside the verification --------------------------------------- */
+
+/*
+ * The drafts of every row: n independent draws from q cut to its k largest tokens and renormalised over them (ties: lower token id), the
+ * support that gr_solve takes for the same q, k and handle; k <= 0 or k >= V: from the whole row.
+ * Draw j is the first token id, in ascending order over the support, at which the running float64 sum of q exceeds uniforms[b, j] times the
+ * support's sum; a token of mass 0 is never drawn.
+ * q           [B, V] float32, row_stride >= V elements from a row to the next, at any alignment.
+ * n           1..max_n of the handle.   uniforms [B, n] float32 in [0, 1).
+ * k           1..GR_MAX_SUPPORT, or none; a top-k between GR_MAX_SUPPORT and V gives GR_EUNSUPPORTED.  On a handle with tail_mass > 0 the support is cut
+ *             as gr_solve cuts it; without a top-k of at most GR_MAX_SUPPORT such a handle gives GR_EUNSUPPORTED.
+ * drafts      [B, n] int32 out.   status [B] int32 out: GR_ROW_OK, or GR_ROW_BAD (NaN or negative entry, a row sum further than 1e-3 from 1, no
+ *             positive entry): the row's drafts are then -1.
+ * Overwrites the handle's selection scratch: the policy of an earlier gr_solve is gone (gr_verify returns GR_ESTATE until the next gr_solve).
+ * Neither allocates nor synchronises.  The same draws come out whatever rows stand beside a row, and from run to run.
+ */
+int gr_draft(gr_handle h, const float* q, long long row_stride, int n, int k, const float* uniforms, int B, int V,
+             int* drafts, int* status, void* hip_stream);
+
+/*
+ * gr_draft for rows given as logits: q = softmax(draft_logits / temperature), in float64 from logits of `dtype` (GR_F32, GR_BF16, GR_F16), never written to
+ * memory.  -inf marks a masked token.  temperature [B] float32, positive and finite.  GR_ROW_BAD: a NaN or +inf entry (or finite ones beyond 1e37), a bad
+ * temperature, a row without an unmasked token.  A handle with tail_mass > 0 gives GR_EUNSUPPORTED, as in gr_solve_logits.
+ */
+int gr_draft_logits(gr_handle h, const void* draft_logits, int dtype, long long row_stride, const float* temperature, int n, int k,
+                    const float* uniforms, int B, int V, int* drafts, int* status, void* hip_stream);
+
+/*
+ * Beam search's selection: of the K V continuations of the K beams of every sequence the M of largest score, in decreasing order.  The score of
+ * token v after beam b is scores[s, b] + log softmax(logits[s, b] / temperature[s])[v], computed in float64 and rounded once; ties go to the lower
+ * beam, within a beam to the larger logit and then the lower token id.
+ * logits      [S, K, V] of `dtype`, row_stride >= V elements from a beam to the next (of the next sequence, too), at any alignment.  -inf: masked.
+ * temperature [S] float32, or NULL for 1.
+ * scores      [S, K] float32: the beams' sums of log probabilities; -inf: the beam is not in use (its row is not read).
+ * finished    [S, K] uint8 or NULL.  A finished beam (not 0) has one continuation, the token eos at its own score; its row is not read.
+ * eos         the token that ends a beam, or -1; with `finished` it must lie in [0, V).
+ * S K rows within the handle's max_B, V within its max_V, 1 <= K, M <= GR_MAX_BEAMS.
+ * out_scores  [S, M] float32, out_parent [S, M] int32 (a beam of the same sequence), out_token [S, M] int32, out_finished [S, M] uint8 or NULL (1: the
+ *             token is eos, so the beam has ended).  Beyond the last continuation: -inf, -1, -1, 0; such a beam is one that is not in use.
+ * status      [S] int32: GR_ROW_OK, or GR_ROW_BAD for a NaN or +inf logit (or finite ones beyond 1e37) of a row that is read, a NaN or +inf score, a temperature that is
+ *             not positive and finite: the sequence's outputs are then -inf, -1, -1, 0.
+ * The outputs must not overlap the inputs.  Overwrites the handle's selection scratch, as gr_draft does; neither allocates nor synchronises; the same from run to run.
+ */
+int gr_beam_select(gr_handle h, const void* logits, int dtype, long long row_stride, const float* temperature, const float* scores,
+                   const unsigned char* finished, int eos, int S, int K, int V, int M, float* out_scores, int* out_parent,
+                   int* out_token, unsigned char* out_finished, int* status, void* hip_stream);
+
+/* Where the states of beams lie, in bytes: element x of token t of head h of slice o of beam row r = s K + b is at
+ *   o outer_stride + h head_stride + r row_stride + t token_stride + x                                  (table == NULL: dense rows of `tokens` tokens)
+ *   o outer_stride + h head_stride + table[r, t / block] row_stride + (t % block) token_stride + x      (pages: row_stride from a block to the next)
+ * Slices are layers, keys and values, whatever lies outside the beams; a state without tokens is one token. */
+typedef struct {
+    long long outer, outer_stride;
+    long long heads, head_stride;
+    long long row_stride;
+    long long tokens, token_stride, token_bytes;   /* tokens: of a dense row (ignored with a table) */
+    int block, width, blocks;                      /* with a table: tokens of a block, entries of a table's row, blocks in the pool */
+} gr_state_layout;
+
+/*
+ * The states of the beams (or draft paths) of a sequence follow their parents: tokens first[s] <= t < length[s] of beam (s, b) become those of
+ * beam (s, parent[s, b]) before the call, for all beams of a sequence at once, in place.  Parents may repeat and cross.
+ * parent      [S, K] int32.  An entry outside 0..K-1 leaves its beam as it is.
+ * first, length  [S] int32 or NULL (0, all tokens); cut to 0..tokens.  Nothing outside is read or written.
+ * table       [S K, width] int32 or NULL.  A page that a beam shares with its parent is left as it is; a page that two beams share must not be one that
+ *             either gets from a third (pages of a common prompt lie below `first`).  Entries outside 0..blocks-1 are skipped.
+ * 1 <= K <= GR_MAX_BEAMS, S <= 65535; strides not below 0, at any alignment; the bytes of different tokens must not overlap.
+ * No handle, no scratch; neither allocates nor synchronises.
+ */
+int gr_beam_reorder(void* state, const gr_state_layout* layout, const int* parent, const int* first, const int* length, const int* table,
+                    int S, int K, void* hip_stream);
+
+/*
+ * The pages of a cache after its requests' lengths have changed, on the GPU: for request r going from lengths[r] to new_lengths[r] tokens, blocks of
+ * `block` tokens each, table[r, j] being the block of tokens j block .. (j + 1) block - 1.
+ * First every request that shrinks (a rejected draft, an end) gives the blocks that it no longer needs to the free stack, in the order of requests and places; then
+ * the growing ones, in order, take theirs from its top.  A request that finds too few blocks or slots, and every growing one behind it, keeps its length
+ * (GR_ROW_NO_ROOM); one with a length below 0 or above width * block, too (GR_ROW_BAD).
+ * table       [R, width] int32, updated: entries of new blocks.  Entries of released blocks stay as they are (they mean nothing from then on).
+ * free_blocks [pool] int32 with free_count [1] int32 blocks in use from its begin: the free stack, updated where it grows; its entries from the new count on
+ *             mean nothing.
+ * out_lengths [R] int32, out_free_count [1] int32: the lengths and the count after the call.
+ * starts      [R + 1] int32: the place of every request's first new token among all new tokens; starts[R] is how many there are.
+ * slots       [slots_capacity] int64: for every new token, in order, table entry * block + place in the block (-1 where the entry is below 0); entries from
+ *             starts[R] on are left as they are.
+ * status      [R] int32.
+ * lengths, new_lengths and free_count are only read, and the out arrays must be others: a decoding loop keeps two sets and swaps them.
+ * 1 <= R <= GR_MAX_REQUESTS, R * width, pool and slots_capacity below 2^31.  No handle, no scratch; one launch; neither allocates nor synchronises.
+ */
+int gr_page_update(const int* lengths, const int* new_lengths, int* table, int* free_blocks, const int* free_count, int R, int width,
+                   int block, int pool, long long slots_capacity, int* out_lengths, int* out_free_count, int* starts, long long* slots,
+                   int* status, void* hip_stream);
 
 /* Test / inspection entry points --------------------------------------------------- */
 

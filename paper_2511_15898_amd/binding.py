@@ -15,18 +15,26 @@ from .build import LIB_PATH
 GR_MAX_SUPPORT = 256
 GR_MAX_T = 128
 GR_MAX_N = 16
-GR_ROW_OK, GR_ROW_TRUNC_CAP, GR_ROW_ITER_CAP, GR_ROW_BAD = 0, 1, 2, 3
+GR_MAX_BEAMS = 64
+GR_MAX_REQUESTS = 8192
+GR_F32, GR_BF16, GR_F16 = 0, 1, 2
+GR_ROW_OK, GR_ROW_TRUNC_CAP, GR_ROW_ITER_CAP, GR_ROW_BAD, GR_ROW_NO_ROOM = 0, 1, 2, 3, 4
 GR_OK, GR_EINVAL, GR_ENOMEM, GR_ESTATE, GR_EHIP, GR_EUNSUPPORTED, GR_ECAPACITY = 0, -1, -2, -3, -4, -5, -6
 GR_NOALLOC_MAX_B = 256
 
 EXPORTS = ("gr_create", "gr_destroy", "gr_solve", "gr_solve_logits", "gr_tree_walk", "gr_profile_stride", "gr_accept_sweep", "gr_accept_sweep_noalloc", "gr_verify", "gr_solve_verify", "gr_solve_logits_verify", "gr_policy_slice", "gr_policy_export",
-           "gr_policy_export_row", "gr_solve_stats", "gr_profile_read", "gr_strerror")
+           "gr_draft", "gr_draft_logits", "gr_beam_select", "gr_beam_reorder", "gr_page_update", "gr_policy_export_row", "gr_solve_stats", "gr_profile_read", "gr_strerror")
 GR_FLAG_PROFILE = 1
 
 
 class GrConfig(ctypes.Structure):
     _fields_ = [("max_iter", ctypes.c_int), ("max_T", ctypes.c_int), ("rel_tol", ctypes.c_double),
                 ("flags", ctypes.c_int), ("tail_mass", ctypes.c_double)]
+
+
+class GrStateLayout(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_longlong) for name in ("outer", "outer_stride", "heads", "head_stride", "row_stride", "tokens", "token_stride", "token_bytes")] + \
+               [(name, ctypes.c_int) for name in ("block", "width", "blocks")]
 
 
 class GrError(RuntimeError):
@@ -59,6 +67,12 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
     lib.gr_solve_verify.argtypes = [vp, vp, vp, ci, ci, ctypes.c_float, ci, ci, vp, vp, vp, vp, vp, vp, vp]
     lib.gr_solve_logits_verify.argtypes = [vp, vp, vp, vp, vp, ci, ci, ctypes.c_float, ci, ci, vp, vp, vp, vp, vp, vp, vp]
     lib.gr_tree_walk.argtypes = [vp, vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, ctypes.c_float, vp, vp, vp, vp, vp]
+    ll = ctypes.c_longlong
+    lib.gr_draft.argtypes = [vp, vp, ll, ci, ci, vp, ci, ci, vp, vp, vp]
+    lib.gr_draft_logits.argtypes = [vp, vp, ci, ll, vp, ci, ci, vp, ci, ci, vp, vp, vp]
+    lib.gr_beam_select.argtypes = [vp, vp, ci, ll, vp, vp, vp, ci, ci, ci, ci, ci, vp, vp, vp, vp, vp, vp]
+    lib.gr_beam_reorder.argtypes = [vp, ctypes.POINTER(GrStateLayout), vp, vp, vp, vp, ci, ci, vp]
+    lib.gr_page_update.argtypes = [vp, vp, vp, vp, vp, ci, ci, ci, ci, ll, vp, vp, vp, vp, vp, vp]
     lib.gr_policy_slice.argtypes = [vp, vp, vp, vp, vp]
     lib.gr_policy_export.argtypes = [vp] * 9
     lib.gr_solve_stats.argtypes = [vp] * 4
@@ -317,6 +331,194 @@ def gr_solve_logits_verify(handle: int, target_logits: torch.Tensor, draft_logit
         raise GrError(rc, "gr_solve_logits_verify")
     _solved_shape[handle] = (B, n, V)
     return accept_prob, status, token, accepted
+
+
+_LOGIT_TYPES = {torch.float32: GR_F32, torch.bfloat16: GR_BF16, torch.float16: GR_F16}
+
+
+def _here(what: str, *tensors) -> None:
+    """All of a call's tensors on the current GPU: the call runs on one of its streams."""
+    current = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != current:
+            raise TypeError(f"{what}: every tensor must be on the current CUDA device {current}, got one on {t.device}")
+
+
+def _shaped(t: torch.Tensor | None, dtype: torch.dtype, shape: tuple, what: str) -> int | None:
+    """The address of a contiguous tensor of just this type and shape."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise TypeError(f"{what}: need a contiguous CUDA tensor of {dtype} and shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _fresh(stream, device, *shapes) -> list:
+    """New tensors for results that `stream` writes, out of memory that no other stream is still using."""
+    current = torch.cuda.current_stream()
+    if stream is None or stream.cuda_stream == current.cuda_stream:
+        return [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in shapes]
+    with torch.cuda.stream(stream):
+        made = [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in shapes]
+    for t in made:
+        t.record_stream(current)
+    return made
+
+
+def _used_on(stream, *tensors) -> int:
+    """The stream's address; tensors that another stream than the current one works on are not given to others before it is done."""
+    current = torch.cuda.current_stream()
+    if stream is None or stream.cuda_stream == current.cuda_stream:
+        return current.cuda_stream
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
+    return stream.cuda_stream
+
+
+def _row_stride(x: torch.Tensor, what: str) -> int:
+    """Elements between the rows of x [..., rows, V]: the entries of a row lie side by side, the rows at one distance."""
+    if x.stride(-1) != 1 and x.shape[-1] > 1:
+        raise TypeError(f"{what}: the entries of a row must lie side by side")
+    stride, rows = None, 1
+    for d in range(x.dim() - 2, -1, -1):
+        if x.shape[d] > 1:
+            if stride is None:
+                stride = x.stride(d) // rows if x.stride(d) % rows == 0 else -1
+            if x.stride(d) != stride * rows or stride < x.shape[-1]:
+                raise TypeError(f"{what}: the rows must lie at one distance, of {x.shape[-1]} elements or more, got strides {tuple(x.stride())}")
+        rows *= x.shape[d]
+    return x.shape[-1] if stride is None else stride
+
+
+def gr_draft(handle: int, q: torch.Tensor, n: int, k: int, uniforms: torch.Tensor, drafts: torch.Tensor | None = None,
+             status: torch.Tensor | None = None, stream=None):
+    """n i.i.d. draws per row from q [B, V] float32 cut to its k largest (k <= 0: the whole row); uniforms [B, n] float32.  The rows of q may lie
+    further apart than V.  Returns (drafts [B, n] int32, status [B] int32)."""
+    if q.dim() != 2 or q.dtype != torch.float32:
+        raise TypeError("gr_draft: q must be [B, V] float32")
+    B, V = q.shape
+    if drafts is None:
+        drafts, = _fresh(stream, q.device, ((B, n), torch.int32))
+    if status is None:
+        status, = _fresh(stream, q.device, ((B,), torch.int32))
+    _here("gr_draft", q, uniforms, drafts, status)
+    rc = load_library().gr_draft(handle, q.data_ptr(), _row_stride(q, "gr_draft"), n, k, _shaped(uniforms, torch.float32, (B, n), "gr_draft: uniforms"), B, V,
+                                 _shaped(drafts, torch.int32, (B, n), "gr_draft: drafts"), _shaped(status, torch.int32, (B,), "gr_draft: status"),
+                                 _used_on(stream, q, uniforms, drafts, status))
+    if rc == GR_OK or rc == GR_EHIP:
+        _solved_shape.pop(handle, None)
+    if rc != GR_OK:
+        raise GrError(rc, "gr_draft")
+    return drafts, status
+
+
+def gr_draft_logits(handle: int, draft_logits: torch.Tensor, temperature: torch.Tensor, n: int, k: int, uniforms: torch.Tensor,
+                    drafts: torch.Tensor | None = None, status: torch.Tensor | None = None, stream=None):
+    """gr_draft for q = softmax(draft_logits / temperature): draft_logits [B, V] float32, bfloat16 or float16, temperature [B] float32."""
+    if draft_logits.dim() != 2 or draft_logits.dtype not in _LOGIT_TYPES:
+        raise TypeError("gr_draft_logits: draft_logits must be [B, V] of float32, bfloat16 or float16")
+    B, V = draft_logits.shape
+    if drafts is None:
+        drafts, = _fresh(stream, draft_logits.device, ((B, n), torch.int32))
+    if status is None:
+        status, = _fresh(stream, draft_logits.device, ((B,), torch.int32))
+    _here("gr_draft_logits", draft_logits, temperature, uniforms, drafts, status)
+    rc = load_library().gr_draft_logits(handle, draft_logits.data_ptr(), _LOGIT_TYPES[draft_logits.dtype], _row_stride(draft_logits, "gr_draft_logits"),
+                                        _shaped(temperature, torch.float32, (B,), "gr_draft_logits: temperature"), n, k,
+                                        _shaped(uniforms, torch.float32, (B, n), "gr_draft_logits: uniforms"), B, V,
+                                        _shaped(drafts, torch.int32, (B, n), "gr_draft_logits: drafts"),
+                                        _shaped(status, torch.int32, (B,), "gr_draft_logits: status"),
+                                        _used_on(stream, draft_logits, temperature, uniforms, drafts, status))
+    if rc == GR_OK or rc == GR_EHIP:
+        _solved_shape.pop(handle, None)
+    if rc != GR_OK:
+        raise GrError(rc, "gr_draft_logits")
+    return drafts, status
+
+
+def gr_beam_select(handle: int, logits: torch.Tensor, scores: torch.Tensor, M: int, temperature: torch.Tensor | None = None,
+                   finished: torch.Tensor | None = None, eos: int = -1, out=None, stream=None):
+    """The M best continuations of the K beams of each of S sequences: logits [S, K, V] float32, bfloat16 or float16 (rows may lie further apart than V),
+    scores [S, K] float32, temperature [S] float32, finished [S, K] uint8.  Returns (scores [S, M] float32, parent [S, M] int32, token [S, M] int32,
+    finished [S, M] uint8, status [S] int32); `out`: the same five tensors to write to."""
+    if logits.dim() != 3 or logits.dtype not in _LOGIT_TYPES:
+        raise TypeError("gr_beam_select: logits must be [S, K, V] of float32, bfloat16 or float16")
+    S, K, V = logits.shape
+    if out is None:
+        out = tuple(_fresh(stream, logits.device, ((S, M), torch.float32), ((S, M), torch.int32), ((S, M), torch.int32), ((S, M), torch.uint8), ((S,), torch.int32)))
+    best, parent, token, over, status = out
+    _here("gr_beam_select", logits, scores, temperature, finished, *out)
+    rc = load_library().gr_beam_select(
+        handle, logits.data_ptr(), _LOGIT_TYPES[logits.dtype], _row_stride(logits, "gr_beam_select"),
+        _shaped(temperature, torch.float32, (S,), "gr_beam_select: temperature"), _shaped(scores, torch.float32, (S, K), "gr_beam_select: scores"),
+        _shaped(finished, torch.uint8, (S, K), "gr_beam_select: finished"), eos, S, K, V, M,
+        _shaped(best, torch.float32, (S, M), "gr_beam_select: out scores"), _shaped(parent, torch.int32, (S, M), "gr_beam_select: out parent"),
+        _shaped(token, torch.int32, (S, M), "gr_beam_select: out token"), _shaped(over, torch.uint8, (S, M), "gr_beam_select: out finished"),
+        _shaped(status, torch.int32, (S,), "gr_beam_select: out status"), _used_on(stream, logits, scores, temperature, finished, *out))
+    if rc == GR_OK or rc == GR_EHIP:
+        _solved_shape.pop(handle, None)
+    if rc != GR_OK:
+        raise GrError(rc, "gr_beam_select")
+    return out
+
+
+def gr_beam_reorder(state: torch.Tensor, parent: torch.Tensor, first: torch.Tensor | None = None, length: torch.Tensor | None = None,
+                    table: torch.Tensor | None = None, stream=None):
+    """The beams' states follow their parents, in place: state [O, S K, H, T, D], or with a block table [S K, width] int32 [O, blocks, H, block, D], of any
+    type and strides (only D lies side by side); parent [S, K] int32; tokens first[s] <= t < length[s] are moved ([S] int32 each).  Returns state."""
+    if state.dim() != 5 or parent.dim() != 2 or 0 in state.shape:
+        raise TypeError("gr_beam_reorder: state must be [O, rows, H, T, D] and parent [S, K]")
+    S, K = parent.shape
+    O, rows, H, T, D = state.shape
+    size = state.element_size()
+    so, sr, sh, st, sd = (x * size for x in state.stride())
+    if sd != size and D > 1:
+        raise TypeError("gr_beam_reorder: the last dimension must lie side by side")
+    if any(x == 0 and n > 1 for x, n in zip((so, sr, sh, st), state.shape)):
+        raise TypeError("gr_beam_reorder: an expanded state cannot be written")
+    layout = GrStateLayout(O, so, H, sh, sr, T, st, D * size, 0, 0, 0)
+    if table is not None:
+        if table.dim() != 2 or table.shape[0] != S * K:
+            raise TypeError("gr_beam_reorder: table must be [S K, width]")
+        layout.block, layout.width, layout.blocks = T, table.shape[1], rows
+    elif rows != S * K:
+        raise TypeError(f"gr_beam_reorder: state has {rows} rows for {S * K} beams")
+    _here("gr_beam_reorder", state, parent, first, length, table)
+    rc = load_library().gr_beam_reorder(state.data_ptr(), layout, _shaped(parent, torch.int32, (S, K), "gr_beam_reorder: parent"),
+                                        _shaped(first, torch.int32, (S,), "gr_beam_reorder: first"),
+                                        _shaped(length, torch.int32, (S,), "gr_beam_reorder: length"),
+                                        None if table is None else _shaped(table, torch.int32, table.shape, "gr_beam_reorder: table"), S, K,
+                                        _used_on(stream, state, parent, first, length, table))
+    if rc != GR_OK:
+        raise GrError(rc, "gr_beam_reorder")
+    return state
+
+
+def gr_page_update(lengths: torch.Tensor, new_lengths: torch.Tensor, table: torch.Tensor, free_blocks: torch.Tensor, free_count: torch.Tensor,
+                   block: int, slots: torch.Tensor, out=None, stream=None):
+    """Block tables, slots and the free stack after lengths [R] -> new_lengths [R] (int32): table [R, width] int32, free_blocks [pool] int32 and slots [capacity]
+    int64 are updated, free_count [1] int32 is read.  Returns (lengths [R], free_count [1], starts [R + 1], status [R]), all int32; `out`: the same four
+    tensors to write to, others than the ones read."""
+    if lengths.dim() != 1 or table.dim() != 2 or free_blocks.dim() != 1 or slots.dim() != 1:
+        raise TypeError("gr_page_update: lengths [R], table [R, width], free_blocks [pool], slots [capacity]")
+    R, width = lengths.shape[0], table.shape[1]
+    if out is None:
+        out = tuple(_fresh(stream, lengths.device, *(((m,), torch.int32) for m in (R, 1, R + 1, R))))
+    after, left, starts, status = out
+    _here("gr_page_update", lengths, new_lengths, table, free_blocks, free_count, slots, *out)
+    i32 = torch.int32
+    rc = load_library().gr_page_update(
+        _shaped(lengths, i32, (R,), "gr_page_update: lengths"), _shaped(new_lengths, i32, (R,), "gr_page_update: new_lengths"),
+        _shaped(table, i32, (R, width), "gr_page_update: table"), _shaped(free_blocks, i32, free_blocks.shape, "gr_page_update: free_blocks"),
+        _shaped(free_count, i32, (1,), "gr_page_update: free_count"), R, width, block, free_blocks.shape[0], slots.shape[0],
+        _shaped(after, i32, (R,), "gr_page_update: out lengths"), _shaped(left, i32, (1,), "gr_page_update: out free_count"),
+        _shaped(starts, i32, (R + 1,), "gr_page_update: out starts"), _shaped(slots, torch.int64, slots.shape, "gr_page_update: slots"),
+        _shaped(status, i32, (R,), "gr_page_update: out status"),
+        _used_on(stream, lengths, new_lengths, table, free_blocks, free_count, slots, *out))
+    if rc != GR_OK:
+        raise GrError(rc, "gr_page_update")
+    return out
 
 
 def gr_policy_slice(handle: int, drafts: torch.Tensor, V: int, stream=None):

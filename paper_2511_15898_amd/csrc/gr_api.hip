@@ -5,7 +5,7 @@
 #include <utility>
 #include <vector>
 
-#include "gr_internal.h"
+#include "gr_paths.h"
 
 using namespace gr;
 
@@ -489,6 +489,112 @@ extern "C" int gr_accept_sweep_noalloc(const float* p, const float* q, const int
     return GR_OK;
 }
 
+// ---- beside the verification: drafts, beams, states, pages (see gr_verify.h)
+namespace {
+
+constexpr size_t element_bytes(int dtype) { return dtype == GR_F32 ? 4 : 2; }
+bool rows_fit(const void* x, int dtype, long long row_stride, int V) {
+    return (dtype == GR_F32 || dtype == GR_BF16 || dtype == GR_F16) && row_stride >= V && reinterpret_cast<uintptr_t>(x) % element_bytes(dtype) == 0;
+}
+// The handle's memory is that of one GPU.
+bool on_device(gr_handle h) { int dev = -1; return hipGetDevice(&dev) == hipSuccess && dev == h->device; }
+
+int draft_rows(gr_handle h, const RowSource& src, bool probs, int n, int k, const float* uniforms, int* drafts, int* status, hipStream_t stream) {
+    if (src.rows <= 0 || src.V <= 0 || src.rows > h->max_B || src.V > h->max_V || n < 1 || n > h->max_n) return GR_EINVAL;
+    if (!rows_fit(src.x, src.dtype, src.stride, src.V) || !on_device(h)) return GR_EINVAL;
+    const bool all = k <= 0 || k >= src.V;
+    const int k_eff = all ? src.V : k;
+    if ((!all && k_eff > kMaxSupport) || (h->tail_mass > 0.0 && (!probs || k_eff > kMaxSupport))) return GR_EUNSUPPORTED;
+    h->solved = false;                                   // the selection scratch of the handle is overwritten
+    const DraftOut out{uniforms, n, drafts, status};
+    if (k_eff <= kMaxSupport) {
+        const RowSlices cut = choose_row_slices(src.rows, src.V, src.dtype, k_eff);
+        const RowParts parts{h->cand, h->cand_count, h->part_psum, h->part_pref, h->part_bad};
+        launch_rows(src, probs, false, k_eff, cut, parts, stream);
+        if (hipGetLastError() != hipSuccess) return GR_EHIP;
+        launch_draft_topk(src, probs, k_eff, h->tail_mass, cut, parts, out, stream);
+    } else {
+        const int pieces = piece_count(src.V, src.dtype);
+        launch_masses(src, probs, pieces, h->piece_stride, h->piece_psum, h->piece_pref, stream);
+        if (hipGetLastError() != hipSuccess) return GR_EHIP;
+        launch_draft_whole(src, probs, pieces, h->piece_stride, h->piece_psum, h->piece_pref, out, stream);
+    }
+    return hipGetLastError() != hipSuccess ? GR_EHIP : GR_OK;
+}
+
+}  // namespace
+
+extern "C" int gr_draft(gr_handle h, const float* q, long long row_stride, int n, int k, const float* uniforms, int B, int V, int* drafts,
+                        int* status, void* hip_stream) {
+    if (!h || !q || !uniforms || !drafts || !status) return GR_EINVAL;
+    const RowSource src{q, GR_F32, row_stride, B, V, nullptr, 1, nullptr, nullptr};
+    return draft_rows(h, src, true, n, k, uniforms, drafts, status, static_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" int gr_draft_logits(gr_handle h, const void* draft_logits, int dtype, long long row_stride, const float* temperature, int n, int k,
+                               const float* uniforms, int B, int V, int* drafts, int* status, void* hip_stream) {
+    if (!h || !draft_logits || !temperature || !uniforms || !drafts || !status) return GR_EINVAL;
+    const RowSource src{draft_logits, dtype, row_stride, B, V, temperature, 1, nullptr, nullptr};
+    return draft_rows(h, src, false, n, k, uniforms, drafts, status, static_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" int gr_beam_select(gr_handle h, const void* logits, int dtype, long long row_stride, const float* temperature, const float* scores,
+                              const unsigned char* finished, int eos, int S, int K, int V, int M, float* out_scores, int* out_parent,
+                              int* out_token, unsigned char* out_finished, int* status, void* hip_stream) {
+    if (!h || !logits || !scores || !out_scores || !out_parent || !out_token || !status) return GR_EINVAL;
+    if (S <= 0 || K < 1 || K > GR_MAX_BEAMS || M < 1 || M > GR_MAX_BEAMS || V <= 0 || V > h->max_V || S > h->max_B / K) return GR_EINVAL;
+    if (eos < -1 || eos >= V || (finished && eos < 0)) return GR_EINVAL;
+    if (!rows_fit(logits, dtype, row_stride, V) || !on_device(h)) return GR_EINVAL;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    h->solved = false;                                   // the selection scratch of the handle is overwritten
+    const RowSource src{logits, dtype, row_stride, S * K, V, temperature, K, scores, finished};
+    const int k = std::min(M, V);
+    const RowSlices cut = choose_row_slices(S * K, V, dtype, k);
+    const RowParts parts{h->cand, h->cand_count, h->part_psum, h->part_pref, h->part_bad};
+    launch_rows(src, false, true, k, cut, parts, stream);
+    if (hipGetLastError() != hipSuccess) return GR_EHIP;
+    launch_beam_merge(src, S, K, M, eos, cut, parts, BeamOut{out_scores, out_parent, out_token, out_finished, status}, stream);
+    return hipGetLastError() != hipSuccess ? GR_EHIP : GR_OK;
+}
+
+extern "C" int gr_beam_reorder(void* state, const gr_state_layout* layout, const int* parent, const int* first, const int* length,
+                               const int* table, int S, int K, void* hip_stream) {
+    if (!state || !layout || !parent) return GR_EINVAL;
+    const gr_state_layout& a = *layout;
+    if (S <= 0 || S > 65535 || K < 1 || K > GR_MAX_BEAMS) return GR_EINVAL;
+    constexpr long long kMost = 0x7FFFFFFF;
+    if (a.outer < 1 || a.heads < 1 || a.outer > kMost / a.heads || a.token_bytes < 1 || a.outer_stride < 0 || a.head_stride < 0 || a.row_stride < 0 || a.token_stride < 0)
+        return GR_EINVAL;
+    ReorderParams rp{};
+    rp.state = static_cast<unsigned char*>(state);
+    rp.outer = a.outer; rp.outer_stride = a.outer_stride; rp.heads = a.heads; rp.head_stride = a.head_stride;
+    rp.token_stride = a.token_stride; rp.token_bytes = a.token_bytes; rp.row_stride = a.row_stride;
+    rp.S = S; rp.K = K; rp.parent = parent; rp.first = first; rp.length = length;
+    if (table) {
+        if (a.block < 1 || a.width < 1 || a.blocks < 1 || static_cast<long long>(a.block) * a.width > kMost || a.block * a.token_bytes > kMost) return GR_EINVAL;
+        rp.table = table; rp.width = a.width; rp.blocks = a.blocks; rp.block = a.block;
+        rp.tokens = static_cast<long long>(a.block) * a.width;
+    } else {
+        if (a.tokens < 1 || a.tokens > kMost || a.token_bytes > kMost) return GR_EINVAL;
+        rp.tokens = a.tokens;
+    }
+    if (K == 1) return GR_OK;                             // a beam alone is its own parent
+    launch_reorder(rp, static_cast<hipStream_t>(hip_stream));
+    return hipGetLastError() != hipSuccess ? GR_EHIP : GR_OK;
+}
+
+extern "C" int gr_page_update(const int* lengths, const int* new_lengths, int* table, int* free_blocks, const int* free_count, int R, int width,
+                              int block, int pool, long long slots_capacity, int* out_lengths, int* out_free_count, int* starts, long long* slots,
+                              int* status, void* hip_stream) {
+    if (!lengths || !new_lengths || !table || !free_blocks || !free_count || !out_lengths || !out_free_count || !starts || !status) return GR_EINVAL;
+    constexpr long long kMost = 0x7FFFFFFF;
+    if (R < 1 || R > GR_MAX_REQUESTS || width < 1 || block < 1 || pool < 1 || slots_capacity < 0 || slots_capacity > kMost || (slots_capacity > 0 && !slots)) return GR_EINVAL;
+    if (static_cast<long long>(R) * width > kMost || static_cast<long long>(width) * block > kMost) return GR_EINVAL;
+    if (out_lengths == lengths || out_lengths == new_lengths || out_free_count == free_count) return GR_EINVAL;
+    const PageParams pp{lengths, new_lengths, table, free_blocks, free_count, R, width, block, pool, slots_capacity, out_lengths, out_free_count, starts, status, slots};
+    return launch_pages(pp, static_cast<hipStream_t>(hip_stream)) != hipSuccess ? hip_failed() : GR_OK;
+}
+
 extern "C" int gr_verify(gr_handle h, const int* drafts, const float* uniforms, int* token,
                          unsigned char* accepted, void* hip_stream) {
     if (!h || !drafts || !uniforms || !token || !accepted) return GR_EINVAL;
@@ -801,7 +907,7 @@ extern "C" const char* gr_strerror(int code) {
         case GR_ENOMEM: return "device allocation failed";
         case GR_ESTATE: return "no solved policy in this handle";
         case GR_EHIP: return "HIP runtime error";
-        case GR_EUNSUPPORTED: return "a vocabulary of 2^24 tokens or more with a support above GR_MAX_SUPPORT, or a dense export of such a policy";
+        case GR_EUNSUPPORTED: return "a vocabulary of 2^24 tokens or more with a support above GR_MAX_SUPPORT, a dense export of such a policy, drafts from a top-k above GR_MAX_SUPPORT, or a nucleus cut of logits";
         case GR_ECAPACITY: return "more rows than GR_NOALLOC_MAX_B, the fixed capacity of the allocation-free entry point";
         default: return "unknown error";
     }

@@ -1,0 +1,307 @@
+// Beams: the choice of the best continuations of a sequence's beams, and the states that follow their beams.
+#include <algorithm>
+
+#include "gr_paths.h"
+
+namespace gr {
+
+namespace {
+
+constexpr int kMergeThreads = 512, kMergeWaves = kMergeThreads / 64, kMergeCap = 1024;
+constexpr int kBatchKeys = kMergeWaves * GR_MAX_BEAMS;    // a wave to a slice's list, at most GR_MAX_BEAMS keys each
+static_assert(kMergeCap >= GR_MAX_BEAMS + kBatchKeys, "a batch always has room behind the best ones");
+constexpr double kNoScore = -__builtin_inf();
+
+struct MergeLds {
+    unsigned long long value[kMergeCap], key[kMergeCap];  // candidates: the score as a rising pattern, (logit, ~id)
+    int beam[kMergeCap];
+    int lists[GR_MAX_BEAMS * kMaxSplits];                 // keys in the list of (beam, slice)
+    double top[GR_MAX_BEAMS], log_sum[GR_MAX_BEAMS], score[GR_MAX_BEAMS];
+    double best[kMergeThreads];
+    int count, bad;
+};
+
+// One candidate before another: by score, then the lower beam, then the larger logit, then the lower id.
+__device__ __forceinline__ bool ahead(unsigned long long va, int ba, unsigned long long ka, unsigned long long vb, int bb, unsigned long long kb) {
+    return va != vb ? va > vb : (ba != bb ? ba < bb : ka > kb);
+}
+
+// The candidates in LDS cut to the best M, in order.
+__device__ void keep_best(MergeLds& L, int c, int M) {
+    const int tid = threadIdx.x;
+    unsigned long long v[kMergeCap / kMergeThreads], k[kMergeCap / kMergeThreads];
+    int b[kMergeCap / kMergeThreads], rank[kMergeCap / kMergeThreads];
+#pragma unroll
+    for (int r = 0; r < kMergeCap / kMergeThreads; ++r) {
+        const int i = tid + r * kMergeThreads;
+        rank[r] = kMergeCap;
+        if (i < c) {
+            v[r] = L.value[i]; k[r] = L.key[i]; b[r] = L.beam[i];
+            int before = 0;
+            for (int j = 0; j < c; ++j) {
+                const unsigned long long vj = L.value[j];
+                if (vj >= v[r]) before += static_cast<int>(ahead(vj, L.beam[j], L.key[j], v[r], b[r], k[r]));
+            }
+            rank[r] = before;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kMergeCap / kMergeThreads; ++r)
+        if (rank[r] < M) { L.value[rank[r]] = v[r]; L.key[rank[r]] = k[r]; L.beam[rank[r]] = b[r]; }
+    if (tid == 0) L.count = min(c, M);
+    __syncthreads();
+}
+
+// grid = (S), 512 threads.  score + (x - top) / T - log sum exp((x' - top) / T), in float64, of every candidate that the slices kept; a lower bound of the
+// M-th best from groups of threads (as in rows_kernel) leaves some dozens, which are put in order by counting.  Bound: a chain of reads behind a launch.
+__global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(const Rows<float> in, int K, int M, int eos, int splits, const RowParts parts, const BeamOut out) {
+    __shared__ MergeLds L;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, seq = blockIdx.x;
+    const int row0 = seq * K;
+    if (tid == 0) { L.count = 0; L.bad = 0; }
+    __syncthreads();
+    const float temp = in.temperature ? in.temperature[seq] : 1.f;
+    const double inv_temp = 1.0 / static_cast<double>(temp);
+    if (tid == 0 && (!(temp > 0.f) || !(temp <= 3.0e38f))) L.bad = 1;
+    for (int b = wave; b < K; b += kMergeWaves) {
+        const int row = row0 + b, at = row * splits + lane;
+        const float score = in.scores[row];
+        const bool skip = in.skip(row), mine = lane < splits && !skip;
+        const int n = mine ? parts.count[at] : 0;
+        if (lane < splits) L.lists[b * splits + lane] = n;
+        const int bad = mine ? parts.bad[at] : 0;
+        const float ref = mine ? parts.ref[at] : kNone;
+        const double sum = mine ? parts.sum[at] : 0.0;
+        const double top = wave_max(static_cast<double>(ref));
+        const double total = wave_sum(ref > kNone ? sum * exp((static_cast<double>(ref) - top) * inv_temp) : 0.0);
+        if (lane == 0) { L.top[b] = top; L.log_sum[b] = log(total); L.score[b] = static_cast<double>(score); }
+        if (__ballot(bad != 0) != 0ull || !(score < 3.0e38f)) if (lane == 0) L.bad = 1;      // any wave that sets it
+    }
+    __syncthreads();
+    const size_t at0 = static_cast<size_t>(seq) * M;
+    if (L.bad) {
+        for (int r = tid; r < M; r += kMergeThreads) {
+            out.scores[at0 + r] = kNone; out.parent[at0 + r] = -1; out.token[at0 + r] = -1;
+            if (out.finished) out.finished[at0 + r] = 0;
+        }
+        if (tid == 0) out.status[seq] = GR_ROW_BAD;
+        return;
+    }
+    const int lists = K * splits, room = kSelCap / splits;
+    // lanes take turns at being the first of a list, so that every group of lanes meets candidates
+    const auto candidate = [&](int list, unsigned long long& key, double& value) -> bool {
+        const int b = list / splits, i = (lane + list * 13) & 63;
+        if (i >= L.lists[list]) return false;
+        key = parts.cand[static_cast<size_t>(row0 + b) * kSelCap + (list - b * splits) * room + i];
+        value = L.score[b] + ((static_cast<double>(key_logit(key)) - L.top[b]) * inv_temp - L.log_sum[b]);
+        return true;
+    };
+    double mine = kNoScore;
+    for (int list = wave; list < lists; list += kMergeWaves) {
+        unsigned long long key; double value;
+        if (candidate(list, key, value)) mine = fmax(mine, value);
+    }
+    int groups = 1;
+    while (groups < M) groups *= 2;
+    for (int o = 32; o >= groups; o >>= 1) mine = fmax(mine, __shfl_xor(mine, o));
+    L.best[tid] = mine;
+    __syncthreads();
+    mine = L.best[lane];
+#pragma unroll
+    for (int w = 1; w < kMergeWaves; ++w) mine = fmax(mine, L.best[lane + 64 * w]);
+    double theta = wave_min(mine);
+    const auto append = [&](double value, unsigned long long key, int b) {
+        const int slot = atomicAdd(&L.count, 1);
+        if (slot < kMergeCap) { L.value[slot] = mono64(value); L.key[slot] = key; L.beam[slot] = b; }
+    };
+    // a finished beam's one candidate
+    const auto append_finished = [&]() {
+        for (int b = tid; b < K; b += kMergeThreads)
+            if (in.finished && in.finished[row0 + b] != 0 && L.score[b] > kNoScore) append(L.score[b], make_key_logit(0.f, eos), b);
+    };
+    append_finished();
+    for (int list = wave; list < lists; list += kMergeWaves) {
+        unsigned long long key; double value;
+        if (candidate(list, key, value) && value >= theta) append(value, key, list / splits);
+    }
+    __syncthreads();
+    int c = L.count;
+    if (c > kMergeCap) {
+        // more than there is room for, equal scores for the most part: a batch of lists at a time behind the best so far
+        __syncthreads();
+        if (tid == 0) L.count = 0;
+        __syncthreads();
+        append_finished();
+        for (int first = 0; first < lists; first += kMergeWaves) {
+            __syncthreads();
+            c = L.count;
+            __syncthreads();
+            if (c > kMergeCap - kBatchKeys) {
+                keep_best(L, c, M);
+                c = min(c, M);
+                if (c == M) theta = fmax(theta, unmono64(L.value[M - 1]));
+                __syncthreads();
+            }
+            const int list = first + wave;
+            unsigned long long key; double value;
+            if (list < lists && candidate(list, key, value) && value >= theta) append(value, key, list / splits);
+        }
+        __syncthreads();
+        c = L.count;
+    }
+    __syncthreads();
+    keep_best(L, c, M);
+    c = min(c, M);
+    for (int r = tid; r < M; r += kMergeThreads) {
+        const bool have = r < c;
+        const int token = have ? key_id(L.key[r]) : -1;
+        out.scores[at0 + r] = have ? static_cast<float>(unmono64(L.value[r])) : kNone;
+        out.parent[at0 + r] = have ? L.beam[r] : -1;
+        out.token[at0 + r] = token;
+        if (out.finished) out.finished[at0 + r] = have && token == eos;
+    }
+    if (tid == 0) out.status[seq] = GR_ROW_OK;
+}
+
+// ---------------------------------------------------------------- states
+
+struct __attribute__((packed, aligned(1))) Any16 { unsigned w[4]; };   // 16 bytes wherever they lie (gfx950 loads and stores them in one instruction)
+
+// The last unit of a stretch, 1 to 15 bytes of it.
+struct __attribute__((packed, aligned(1))) Any8 { unsigned w[2]; };
+struct __attribute__((packed, aligned(1))) Any4 { unsigned w; };
+struct __attribute__((packed, aligned(1))) Any2 { unsigned short w; };
+__device__ __forceinline__ Any16 load_part(const unsigned char* p, int bytes) {
+    Any16 v = {};
+    if (bytes & 8) { const Any8 x = *reinterpret_cast<const Any8*>(p); v.w[0] = x.w[0]; v.w[1] = x.w[1]; p += 8; }
+    if (bytes & 4) { v.w[2] = reinterpret_cast<const Any4*>(p)->w; p += 4; }
+    if (bytes & 2) { v.w[3] = reinterpret_cast<const Any2*>(p)->w; p += 2; }
+    if (bytes & 1) v.w[3] |= static_cast<unsigned>(*p) << 16;
+    return v;
+}
+__device__ __forceinline__ void store_part(unsigned char* p, int bytes, const Any16& v) {
+    if (bytes & 8) { Any8 x; x.w[0] = v.w[0]; x.w[1] = v.w[1]; *reinterpret_cast<Any8*>(p) = x; p += 8; }
+    if (bytes & 4) { reinterpret_cast<Any4*>(p)->w = v.w[2]; p += 4; }
+    if (bytes & 2) { reinterpret_cast<Any2*>(p)->w = static_cast<unsigned short>(v.w[3]); p += 2; }
+    if (bytes & 1) *p = static_cast<unsigned char>(v.w[3] >> 16);
+}
+
+// grid = (chunks of tokens, sequences, groups of slices), 256 threads; a slice is an (outer index, head).
+// In place, so a beam may be read for one and written for another: a thread reads all that its 16 bytes of the beams need before it writes any, and no
+// other thread touches them.  W: steps of 256 units that are in flight at once; N W loads per thread, 16 of them, fill the chip's memory pipes.
+// Bound: HBM; every row that another beam takes is read from it once (a second taker finds it in L2), every row whose parent is another is written.
+template <int N, int W>
+__global__ __launch_bounds__(kThreads) void reorder_kernel(const ReorderParams rp, int per_group) {
+    __shared__ long long from_row[N], to_row[N];
+    __shared__ int moves_shared;
+    const int tid = threadIdx.x, chunk = blockIdx.x, seq = blockIdx.y;
+    const long long t_first = static_cast<long long>(chunk) * rp.block;
+    const long long len = rp.length ? rp.length[seq] * rp.scale : rp.tokens, lo = rp.first ? rp.first[seq] * rp.scale : 0;
+    const long long t0 = max(max(lo, 0ll), t_first), t1 = min(min(len, rp.tokens), t_first + rp.block);
+    if (t0 >= t1) return;
+    if (tid < 64) {
+        long long from = 0, to = 0;
+        bool move = false;
+        if (tid < rp.K) {
+            const int row = seq * rp.K + tid, parent = rp.parent[row];
+            move = parent >= 0 && parent < rp.K && parent != tid;
+            if (move) {
+                if (rp.table) {
+                    const int a = rp.table[static_cast<long long>(seq * rp.K + parent) * rp.width + chunk], b = rp.table[static_cast<long long>(row) * rp.width + chunk];
+                    move = a != b && a >= 0 && a < rp.blocks && b >= 0 && b < rp.blocks;       // a page that the two share stays as it is
+                    from = a * rp.row_stride; to = b * rp.row_stride;
+                } else {
+                    from = static_cast<long long>(seq * rp.K + parent) * rp.row_stride + t_first * rp.token_stride;
+                    to = static_cast<long long>(row) * rp.row_stride + t_first * rp.token_stride;
+                }
+            }
+        }
+        const unsigned long long all = __ballot(move);
+        if (move) { const int at = __popcll(all & ((1ull << tid) - 1ull)); from_row[at] = from; to_row[at] = to; }
+        if (tid == 0) moves_shared = __popcll(all);
+    }
+    __syncthreads();
+    const int moves = __builtin_amdgcn_readfirstlane(moves_shared);
+    if (moves == 0) return;
+    // the stretch of a row: `segments` tokens of seg bytes, one if they lie one after the other
+    const bool joined = rp.token_stride == rp.token_bytes;
+    const long long skip = (t0 - t_first) * rp.token_stride;
+    const long long seg = joined ? (t1 - t0) * rp.token_bytes : rp.token_bytes;
+    const int segments = joined ? 1 : static_cast<int>(t1 - t0);
+    const int per_seg = static_cast<int>((seg + 15) / 16), units = per_seg * segments, rounds = (units + kThreads - 1) / kThreads;
+    const unsigned heads = static_cast<unsigned>(rp.heads), q0 = blockIdx.z * static_cast<unsigned>(per_group);
+    const int steps = min(per_group, static_cast<int>(static_cast<unsigned>(rp.outer) * heads - q0)) * rounds;
+    for (int step = 0; step < steps; step += W) {
+        long long off[W]; int bytes[W];
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const int st = step + w, qi = st / rounds, u = (st - qi * rounds) * kThreads + tid;
+            const unsigned q = q0 + qi, o = q / heads, h = q - o * heads;
+            const int sg = segments == 1 ? 0 : u / per_seg, i = u - sg * per_seg;
+            off[w] = o * rp.outer_stride + h * rp.head_stride + skip + sg * rp.token_stride + static_cast<long long>(i) * 16;
+            bytes[w] = st < steps && u < units ? static_cast<int>(min(16ll, seg - static_cast<long long>(i) * 16)) : 0;
+        }
+        Any16 v[W][N];
+#pragma unroll
+        for (int m = 0; m < N; ++m)
+            if (m < moves) {
+                const long long from = from_row[m];
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    const unsigned char* const p = rp.state + from + off[w];
+                    if (bytes[w] == 16) v[w][m] = *reinterpret_cast<const Any16*>(p);
+                    else if (bytes[w] > 0) v[w][m] = load_part(p, bytes[w]);
+                }
+            }
+#pragma unroll
+        for (int m = 0; m < N; ++m)
+            if (m < moves) {
+                const long long to = to_row[m];
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    unsigned char* const p = rp.state + to + off[w];
+                    if (bytes[w] == 16) *reinterpret_cast<Any16*>(p) = v[w][m];
+                    else if (bytes[w] > 0) store_part(p, bytes[w], v[w][m]);
+                }
+            }
+    }
+}
+
+}  // namespace
+
+void launch_beam_merge(const RowSource& src, int S, int K, int M, int eos, RowSlices cut, const RowParts& in, const BeamOut& out, hipStream_t stream) {
+    hipLaunchKernelGGL(beam_merge_kernel, dim3(S), dim3(kMergeThreads), 0, stream, Rows<float>(src), K, M, eos, cut.splits, in, out);
+}
+
+void launch_reorder(const ReorderParams& params, hipStream_t stream) {
+    ReorderParams rp = params;
+    // heads that lie side by side in a token are part of it
+    if (rp.heads > 1 && rp.head_stride == rp.token_bytes && rp.token_stride == rp.heads * rp.token_bytes) { rp.token_bytes = rp.token_stride; rp.heads = 1; rp.head_stride = 0; }
+    const long long slices = rp.outer * rp.heads;
+    if (rp.tokens == 1) rp.token_stride = rp.token_bytes;
+    rp.scale = 1;
+    if (!rp.table && rp.token_stride == rp.token_bytes) {
+        // a dense row whose tokens lie one after the other is so many bytes
+        rp.scale = rp.token_bytes;
+        rp.tokens *= rp.scale;
+        rp.token_bytes = rp.token_stride = 1;
+    }
+    // a chunk of a dense row: 16 KB, four rounds of a workgroup
+    if (!rp.table) rp.block = static_cast<int>(std::min(std::max(1ll, 16384 / rp.token_bytes), rp.tokens));
+    const int chunks = static_cast<int>((rp.tokens + rp.block - 1) / rp.block);
+    // slices to a workgroup: the moves and the table's entries are looked up once for all of them, but the chip wants some thousands of workgroups
+    const long long units = (static_cast<long long>(rp.block) * rp.token_bytes + 16 * kThreads - 1) / (16 * kThreads);
+    long long per_group = std::max(1ll, 16 / units);
+    per_group = std::min(per_group, std::max(1ll, slices * chunks * rp.S / 4096));
+    per_group = std::max(per_group, (slices + 65534) / 65535);
+    const dim3 grid(chunks, rp.S, static_cast<unsigned>((slices + per_group - 1) / per_group));
+    const int pg = static_cast<int>(per_group);
+    if (rp.K <= 4) hipLaunchKernelGGL((reorder_kernel<4, 4>), grid, dim3(kThreads), 0, stream, rp, pg);
+    else if (rp.K <= 8) hipLaunchKernelGGL((reorder_kernel<8, 2>), grid, dim3(kThreads), 0, stream, rp, pg);
+    else if (rp.K <= 16) hipLaunchKernelGGL((reorder_kernel<16, 1>), grid, dim3(kThreads), 0, stream, rp, pg);
+    else if (rp.K <= 32) hipLaunchKernelGGL((reorder_kernel<32, 1>), grid, dim3(kThreads), 0, stream, rp, pg);
+    else hipLaunchKernelGGL((reorder_kernel<64, 1>), grid, dim3(kThreads), 0, stream, rp, pg);
+}
+
+}  // namespace gr
