@@ -508,9 +508,9 @@ int draft_rows(gr_handle h, const RowSource& src, bool probs, int n, int k, cons
     h->solved = false;                                   // the selection scratch of the handle is overwritten
     const DraftOut out{uniforms, n, drafts, status};
     if (k_eff <= kMaxSupport) {
-        const RowSlices cut = choose_row_slices(src.rows, src.V, src.dtype, k_eff);
+        const RowSlices cut = choose_row_slices(src.rows, src.V, src.dtype, k_eff, false);
         const RowParts parts{h->cand, h->cand_count, h->part_psum, h->part_pref, h->part_bad};
-        launch_rows(src, probs, false, k_eff, cut, parts, stream);
+        launch_rows(src, probs, false, k_eff, kSelCap, cut, parts, stream);
         if (hipGetLastError() != hipSuccess) return GR_EHIP;
         launch_draft_topk(src, probs, k_eff, h->tail_mass, cut, parts, out, stream);
     } else {
@@ -549,9 +549,9 @@ extern "C" int gr_beam_select(gr_handle h, const void* logits, int dtype, long l
     h->solved = false;                                   // the selection scratch of the handle is overwritten
     const RowSource src{logits, dtype, row_stride, S * K, V, temperature, K, scores, finished};
     const int k = std::min(M, V);
-    const RowSlices cut = choose_row_slices(S * K, V, dtype, k);
+    const RowSlices cut = choose_row_slices(S * K, V, dtype, k, true);
     const RowParts parts{h->cand, h->cand_count, h->part_psum, h->part_pref, h->part_bad};
-    launch_rows(src, false, true, k, cut, parts, stream);
+    launch_rows(src, false, true, k, GR_MAX_BEAMS, cut, parts, stream);
     if (hipGetLastError() != hipSuccess) return GR_EHIP;
     launch_beam_merge(src, S, K, M, eos, cut, parts, BeamOut{out_scores, out_parent, out_token, out_finished, status}, stream);
     return hipGetLastError() != hipSuccess ? GR_EHIP : GR_OK;

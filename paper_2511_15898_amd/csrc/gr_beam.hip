@@ -8,6 +8,8 @@ namespace gr {
 namespace {
 
 constexpr int kMergeThreads = 512, kMergeWaves = kMergeThreads / 64, kMergeCap = 1024;
+constexpr int kMaxLists = GR_MAX_BEAMS * kMaxSplits;
+constexpr int kHeldLists = 8;                             // lists of a wave whose keys are on their way at once
 constexpr int kBatchKeys = kMergeWaves * GR_MAX_BEAMS;    // a wave to a slice's list, at most GR_MAX_BEAMS keys each
 static_assert(kMergeCap >= GR_MAX_BEAMS + kBatchKeys, "a batch always has room behind the best ones");
 constexpr double kNoScore = -__builtin_inf();
@@ -15,7 +17,8 @@ constexpr double kNoScore = -__builtin_inf();
 struct MergeLds {
     unsigned long long value[kMergeCap], key[kMergeCap];  // candidates: the score as a rising pattern, (logit, ~id)
     int beam[kMergeCap];
-    int lists[GR_MAX_BEAMS * kMaxSplits];                 // keys in the list of (beam, slice)
+    int lists[kMaxLists];                                 // keys in the list of (beam, slice)
+    float refs[kMaxLists]; double sums[kMaxLists];
     double top[GR_MAX_BEAMS], log_sum[GR_MAX_BEAMS], score[GR_MAX_BEAMS];
     double best[kMergeThreads];
     int count, bad;
@@ -26,58 +29,78 @@ __device__ __forceinline__ bool ahead(unsigned long long va, int ba, unsigned lo
     return va != vb ? va > vb : (ba != bb ? ba < bb : ka > kb);
 }
 
-// The candidates in LDS cut to the best M, in order.
+// The candidates in LDS cut to the best M, in order, by counting; `parts` threads side by side to a candidate where there are few.
 __device__ void keep_best(MergeLds& L, int c, int M) {
     const int tid = threadIdx.x;
-    unsigned long long v[kMergeCap / kMergeThreads], k[kMergeCap / kMergeThreads];
-    int b[kMergeCap / kMergeThreads], rank[kMergeCap / kMergeThreads];
+    constexpr int kEach = kMergeCap / kMergeThreads;
+    unsigned long long v[kEach] = {}, k[kEach] = {};
+    int b[kEach] = {}, rank[kEach];
+    int parts = 1;
+    while (parts < 64 && c * parts * 2 <= kMergeThreads) parts *= 2;
+    const int part = tid % parts;
 #pragma unroll
-    for (int r = 0; r < kMergeCap / kMergeThreads; ++r) {
-        const int i = tid + r * kMergeThreads;
+    for (int r = 0; r < kEach; ++r) {
+        const int i = (tid + r * kMergeThreads) / parts;
         rank[r] = kMergeCap;
-        if (i < c) {
-            v[r] = L.value[i]; k[r] = L.key[i]; b[r] = L.beam[i];
-            int before = 0;
-            for (int j = 0; j < c; ++j) {
-                const unsigned long long vj = L.value[j];
-                if (vj >= v[r]) before += static_cast<int>(ahead(vj, L.beam[j], L.key[j], v[r], b[r], k[r]));
+        if (r > 0 && i >= c) break;                       // with more than one part a second round has nobody
+        if (i < c) { v[r] = L.value[i]; k[r] = L.key[i]; b[r] = L.beam[i]; }
+        int before = 0;
+        for (int j0 = part; j0 < c; j0 += 8 * parts) {
+            unsigned long long other[8];                  // eight reads on their way at once
+#pragma unroll
+            for (int u = 0; u < 8; ++u) other[u] = L.value[min(j0 + u * parts, c - 1)];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int j = j0 + u * parts;
+                if (j < c && other[u] >= v[r]) before += static_cast<int>(ahead(other[u], L.beam[j], L.key[j], v[r], b[r], k[r]));
             }
-            rank[r] = before;
         }
+        for (int o = 1; o < parts; o <<= 1) before += __shfl_xor(before, o);
+        if (i < c && part == 0) rank[r] = before;
     }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kMergeCap / kMergeThreads; ++r)
+    for (int r = 0; r < kEach; ++r)
         if (rank[r] < M) { L.value[rank[r]] = v[r]; L.key[rank[r]] = k[r]; L.beam[rank[r]] = b[r]; }
     if (tid == 0) L.count = min(c, M);
     __syncthreads();
 }
 
 // grid = (S), 512 threads.  score + (x - top) / T - log sum exp((x' - top) / T), in float64, of every candidate that the slices kept; a lower bound of the
-// M-th best from groups of threads (as in rows_kernel) leaves some dozens, which are put in order by counting.  Bound: a chain of reads behind a launch.
+// M-th best, from groups of threads, leaves some dozens, which are put in order by counting.
+// Bound: a chain of steps behind one read.  What the slices left lies in other chips' L2, a microsecond away, so counts, sums and keys are all asked for at the
+// beginning, keys before it is known how many there are (each list after the other took 25 us for 64 lists).
 __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(const Rows<float> in, int K, int M, int eos, int splits, const RowParts parts, const BeamOut out) {
     __shared__ MergeLds L;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, seq = blockIdx.x;
-    const int row0 = seq * K;
+    const int row0 = seq * K, lists = K * splits, room = kSelCap / splits, most = min(room, GR_MAX_BEAMS);
+    // lanes take turns at being the first of a list, so that every group of lanes meets candidates
+    const auto place = [&](int list) { return (lane + list * 13) & 63; };
+    const auto load_key = [&](int list) -> unsigned long long {
+        const int b = list / splits, i = place(list);
+        return list < lists && i < most ? parts.cand[static_cast<size_t>(row0 + b) * kSelCap + (list - b * splits) * room + i] : 0ull;
+    };
+    unsigned long long held[kHeldLists];                  // of lists wave, wave + 8, ..
+#pragma unroll
+    for (int u = 0; u < kHeldLists; ++u) held[u] = load_key(wave + u * kMergeWaves);
+    const float temp = in.temperature ? in.temperature[seq] : 1.f;
     if (tid == 0) { L.count = 0; L.bad = 0; }
     __syncthreads();
-    const float temp = in.temperature ? in.temperature[seq] : 1.f;
-    const double inv_temp = 1.0 / static_cast<double>(temp);
-    if (tid == 0 && (!(temp > 0.f) || !(temp <= 3.0e38f))) L.bad = 1;
-    for (int b = wave; b < K; b += kMergeWaves) {
-        const int row = row0 + b, at = row * splits + lane;
-        const float score = in.scores[row];
-        const bool skip = in.skip(row), mine = lane < splits && !skip;
-        const int n = mine ? parts.count[at] : 0;
-        if (lane < splits) L.lists[b * splits + lane] = n;
-        const int bad = mine ? parts.bad[at] : 0;
-        const float ref = mine ? parts.ref[at] : kNone;
-        const double sum = mine ? parts.sum[at] : 0.0;
-        const double top = wave_max(static_cast<double>(ref));
-        const double total = wave_sum(ref > kNone ? sum * exp((static_cast<double>(ref) - top) * inv_temp) : 0.0);
-        if (lane == 0) { L.top[b] = top; L.log_sum[b] = log(total); L.score[b] = static_cast<double>(score); }
-        if (__ballot(bad != 0) != 0ull || !(score < 3.0e38f)) if (lane == 0) L.bad = 1;      // any wave that sets it
+    for (int i = tid; i < lists; i += kMergeThreads) {
+        const int b = i / splits, at = row0 * splits + i;
+        const bool skip = in.skip(row0 + b);
+        L.lists[i] = skip ? 0 : parts.count[at];
+        L.refs[i] = skip ? kNone : parts.ref[at];
+        L.sums[i] = skip ? 0.0 : parts.sum[at];
+        if (!skip && parts.bad[at] != 0) L.bad = 1;       // any thread that sets it
     }
+    if (tid < K) {
+        const float score = in.scores[row0 + tid];
+        L.score[tid] = static_cast<double>(score);
+        if (!(score < 3.0e38f)) L.bad = 1;
+    }
+    if (tid == 0 && (!(temp > 0.f) || !(temp <= 3.0e38f))) L.bad = 1;
+    const double inv_temp = 1.0 / static_cast<double>(temp);
     __syncthreads();
     const size_t at0 = static_cast<size_t>(seq) * M;
     if (L.bad) {
@@ -88,20 +111,44 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(const Rows<fl
         if (tid == 0) out.status[seq] = GR_ROW_BAD;
         return;
     }
-    const int lists = K * splits, room = kSelCap / splits;
-    // lanes take turns at being the first of a list, so that every group of lanes meets candidates
-    const auto candidate = [&](int list, unsigned long long& key, double& value) -> bool {
-        const int b = list / splits, i = (lane + list * 13) & 63;
-        if (i >= L.lists[list]) return false;
-        key = parts.cand[static_cast<size_t>(row0 + b) * kSelCap + (list - b * splits) * room + i];
+    // the slices' sums to the beam's largest reference: a thread to a slice
+    for (int i = tid; i < lists; i += kMergeThreads) {
+        const int b = i / splits;
+        float top = kNone;
+        for (int s = 0; s < splits; ++s) top = fmaxf(top, L.refs[b * splits + s]);
+        const float ref = L.refs[i];
+        L.sums[i] *= ref > kNone ? exp((static_cast<double>(ref) - static_cast<double>(top)) * inv_temp) : 0.0;
+        if (i == b * splits) L.top[b] = static_cast<double>(top);
+    }
+    __syncthreads();
+    if (tid < K) {
+        double sum = 0.0;
+        for (int s = 0; s < splits; ++s) sum += L.sums[tid * splits + s];
+        L.log_sum[tid] = log(sum);
+    }
+    __syncthreads();
+    const auto candidate = [&](int list, unsigned long long key, double& value) -> bool {
+        if (list >= lists || place(list) >= L.lists[list]) return false;
+        const int b = list / splits;
         value = L.score[b] + ((static_cast<double>(key_logit(key)) - L.top[b]) * inv_temp - L.log_sum[b]);
         return true;
     };
+    // calls use(list, key, value) for every candidate of lists from `first` on, `count` of them
+    const auto each = [&](int first, int count, auto&& use) {
+        for (int l0 = first; l0 < first + count; l0 += kHeldLists * kMergeWaves) {
+            if (first != 0 || l0 != 0 || lists > kHeldLists * kMergeWaves)
+#pragma unroll
+                for (int u = 0; u < kHeldLists; ++u) held[u] = load_key(l0 + wave + u * kMergeWaves);
+#pragma unroll
+            for (int u = 0; u < kHeldLists; ++u) {
+                const int list = l0 + wave + u * kMergeWaves;
+                double value;
+                if (list < first + count && candidate(list, held[u], value)) use(list, held[u], value);
+            }
+        }
+    };
     double mine = kNoScore;
-    for (int list = wave; list < lists; list += kMergeWaves) {
-        unsigned long long key; double value;
-        if (candidate(list, key, value)) mine = fmax(mine, value);
-    }
+    each(0, lists, [&](int, unsigned long long, double value) { mine = fmax(mine, value); });
     int groups = 1;
     while (groups < M) groups *= 2;
     for (int o = 32; o >= groups; o >>= 1) mine = fmax(mine, __shfl_xor(mine, o));
@@ -117,14 +164,10 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(const Rows<fl
     };
     // a finished beam's one candidate
     const auto append_finished = [&]() {
-        for (int b = tid; b < K; b += kMergeThreads)
-            if (in.finished && in.finished[row0 + b] != 0 && L.score[b] > kNoScore) append(L.score[b], make_key_logit(0.f, eos), b);
+        if (tid < K && in.finished && in.finished[row0 + tid] != 0 && L.score[tid] > kNoScore) append(L.score[tid], make_key_logit(0.f, eos), tid);
     };
     append_finished();
-    for (int list = wave; list < lists; list += kMergeWaves) {
-        unsigned long long key; double value;
-        if (candidate(list, key, value) && value >= theta) append(value, key, list / splits);
-    }
+    each(0, lists, [&](int list, unsigned long long key, double value) { if (value >= theta) append(value, key, list / splits); });
     __syncthreads();
     int c = L.count;
     if (c > kMergeCap) {
@@ -144,8 +187,9 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(const Rows<fl
                 __syncthreads();
             }
             const int list = first + wave;
-            unsigned long long key; double value;
-            if (list < lists && candidate(list, key, value) && value >= theta) append(value, key, list / splits);
+            const unsigned long long key = load_key(list);
+            double value;
+            if (candidate(list, key, value) && value >= theta) append(value, key, list / splits);
         }
         __syncthreads();
         c = L.count;

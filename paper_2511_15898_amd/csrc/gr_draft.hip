@@ -10,17 +10,32 @@ namespace gr {
 
 namespace {
 
+constexpr int kDraftThreads = 512, kDraftWaves = kDraftThreads / 64;
+constexpr int kPaddedSupport = 2 * kMaxSupport;           // candidates ranked at once, with what pads them to 8 `parts`; the scan's 64 behind a support
+
 struct DraftLds {
     unsigned long long keys[kSelCap];
-    double mass[kMaxSupport + 64], sum[kMaxSupport + 64 + 1], tmp[kMaxSupport];
-    int ids[kMaxSupport], sorted[kMaxSupport], hist[256], pick[4], count, keep;
+    double mass[kPaddedSupport], sum[kPaddedSupport + 1];
+    int ids[kPaddedSupport], hist[256], pick[4], count;
+    float edge[2 * kDraftWaves];
 };
 
-// grid = (rows), 256 threads.
+// grid = (rows), 512 threads.  The candidates are thinned to 512 at most, ranked by counting and so put in order, best first; a token's CDF is the sum of the
+// masses of the tokens up to its id, added in that order whatever the slices' order was.  Sums of more masses in one order are never smaller, so the CDF
+// rises with the id, and where nothing is added it stays the same: no sort by id and no scan is needed.
 template <bool PROBS>
-__global__ __launch_bounds__(kThreads) void draft_topk_kernel(const float* __restrict__ temperature, int k, double tail_mass, int splits, const RowParts in, const DraftOut out) {
+__global__ __launch_bounds__(kDraftThreads) void draft_topk_kernel(const float* __restrict__ temperature, int k, double tail_mass, int splits, const RowParts in, const DraftOut out) {
     __shared__ DraftLds L;
-    const int tid = threadIdx.x, row = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, row = blockIdx.x, room = kSelCap / splits;
+    // the keys are asked for before it is known how many there are: what lies behind them is the handle's, too, and is not used
+    constexpr int kAhead = kSelCap / kDraftThreads;
+    const unsigned long long* const cand = in.cand + static_cast<size_t>(row) * kSelCap;
+    unsigned long long ahead[kAhead];
+#pragma unroll
+    for (int r = 0; r < kAhead; ++r) {
+        const int i = r * kDraftThreads + tid;
+        ahead[r] = i < splits * room ? cand[i] : 0ull;
+    }
     const SliceTotals found = slice_totals<false>(in.count, in.bad, in.sum, in.sum, nullptr, row, splits, 0.0);
     bool bad = found.bad != 0 || found.total == 0;
     double inv_temp = 1.0;
@@ -34,68 +49,83 @@ __global__ __launch_bounds__(kThreads) void draft_topk_kernel(const float* __res
         if (tid == 0) out.status[row] = GR_ROW_BAD;
         return;
     }
-    gather_keys<kThreads>(L.keys, in.cand + static_cast<size_t>(row) * kSelCap, found, splits);
-    if (tid == 0) L.count = 0;
-    __syncthreads();
-    const int total = found.total;
-    unsigned long long theta = 0ull;
-    if (total > k) theta = block_kth_largest(L.keys, total, k, L.hist, L.pick);
-    int kk = min(total, k);
-    for (int i = tid; i < total; i += kThreads) {
-        const unsigned long long key = L.keys[i];
-        if (key >= theta) {
-            const int slot = atomicAdd(&L.count, 1);      // in any order: they are sorted by id below
-            if (slot < kMaxSupport) { L.ids[slot] = key_id(key); L.tmp[slot] = static_cast<double>(PROBS ? key_q(key) : key_logit(key)); }
-        }
+#pragma unroll
+    for (int r = 0; r < kAhead; ++r) {
+        const int i = r * kDraftThreads + tid, s = min(i / room, splits - 1), at = i - s * room;
+        const int count = __shfl(found.count, s), before = __shfl(found.before, s);
+        if (at < count) L.keys[before + at] = ahead[r];   // at < room: i lies in slice s (behind the last one none counts)
     }
     __syncthreads();
-    int id = tid < kk ? L.ids[tid] : 0x7FFFFFFF;
-    double value = tid < kk ? L.tmp[tid] : 0.0;
-    bool stay = tid < kk;
+    int c = found.total;
+    if (c > 2 * k + 32 || c > kPaddedSupport) c = thin_keys<kSelCap, PROBS, kDraftThreads>(L.keys, c, k, kPaddedSupport, L.hist, L.pick, L.edge, &L.count);
+    // `parts` threads to a candidate, side by side
+    int parts = 1;
+    while (parts < 64 && c * parts * 2 <= kDraftThreads) parts *= 2;
+    const int me = tid / parts, part = tid % parts;
+    const unsigned long long mine = me < c ? L.keys[me] : 0ull;
+    // eight reads on their way at once: one after the other they cost 200 cycles each
+    const int step = 8 * parts, padded = (c + step - 1) / step * step;
+    for (int i = c + tid; i < padded; i += kDraftThreads) L.keys[i] = 0ull;
+    __syncthreads();
+    int rank = 0;
+    for (int j = part; j < padded; j += step) {
+        unsigned long long key[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) key[u] = L.keys[j + u * parts];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) rank += static_cast<int>(key[u] > mine);
+    }
+    for (int o = 1; o < parts; o <<= 1) rank += __shfl_xor(rank, o);
+    __syncthreads();
+    int kk = min(c, k);
+    if (me < c && part == 0 && rank < kk) L.keys[rank] = mine;
+    __syncthreads();
     if (PROBS && tail_mass > 0.0) {
-        // the nucleus cut of gr_solve: by decreasing q (ties by id), up to the first token at which the running sum, added one after the other,
-        // reaches (1 - tail_mass) of the row's mass
-        int rank = 0;
-        if (stay) for (int j = 0; j < kk; ++j) rank += static_cast<int>(L.tmp[j] > value) | (static_cast<int>(L.tmp[j] == value) & static_cast<int>(L.ids[j] < id));
-        if (stay) L.mass[rank] = value;
-        if (tid < 64) L.mass[kk + tid] = 0.0;
+        // the nucleus cut of gr_solve: up to the first token at which the running sum, added one after the other, reaches (1 - tail_mass) of the row's mass
+        if (tid < kk) L.mass[tid] = static_cast<double>(key_q(L.keys[tid]));
+        if (tid < 64) L.mass[kk + tid] = 0.0;             // the scan reads up to a multiple of 64
+        if (tid == 0) L.count = kk;
         __syncthreads();
         if (tid < 64) wave_sequential_scan_padded(L.mass, L.sum, kk, 0.0);
-        if (tid == 0) L.keep = kk;
         __syncthreads();
-        if (stay && L.sum[tid + 1] >= (1.0 - tail_mass) * found.qtot) atomicMin(&L.keep, tid + 1);
+        if (tid < kk && L.sum[tid + 1] >= (1.0 - tail_mass) * found.qtot) atomicMin(&L.count, tid + 1);
         __syncthreads();
-        stay = stay && rank < L.keep;
-        if (tid < kk && !stay) L.ids[tid] = 0x7FFFFFFF;   // behind every id that stays
-        kk = L.keep;
-        __syncthreads();
+        kk = L.count;
     }
-    const int listed = min(total, k);
-    if (!PROBS) {
-        double most = stay ? value : -1e300;
-        most = wave_max(most);
-        if ((tid & 63) == 0) L.sum[tid >> 6] = most;
-        __syncthreads();
-        most = fmax(fmax(L.sum[0], L.sum[1]), fmax(L.sum[2], L.sum[3]));
-        value = exp((value - most) * inv_temp);
+    for (int i = kk + tid; i < padded; i += kDraftThreads) { L.ids[i] = 0; L.mass[i] = 0.0; }
+    if (tid < kk) {
+        const unsigned long long key = L.keys[tid];
+        L.ids[tid] = key_id(key);
+        L.mass[tid] = PROBS ? static_cast<double>(key_q(key)) : exp((static_cast<double>(key_logit(key)) - static_cast<double>(key_logit(L.keys[0]))) * inv_temp);
     }
-    if (stay) {
-        int rank = 0;
-#pragma unroll 8
-        for (int j = 0; j < listed; ++j) rank += static_cast<int>(L.ids[j] < id);
-        L.sorted[rank] = id; L.mass[rank] = value;
-    }
-    if (tid < 64) L.mass[kk + tid] = 0.0;                 // behind the last: the scan reads up to a multiple of 64
     __syncthreads();
-    if (tid < 64) wave_sequential_scan_padded(L.mass, L.sum, kk, 0.0);
+    const int id = me < kk ? L.ids[me] : -1;
+    double upto = 0.0;
+    for (int j = part; j < padded; j += step) {
+        int ids[8]; double mass[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) { ids[u] = L.ids[j + u * parts]; mass[u] = L.mass[j + u * parts]; }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) upto += ids[u] <= id ? mass[u] : 0.0;
+    }
+    for (int o = 1; o < parts; o <<= 1) upto += __shfl_xor(upto, o);
+    if (me < kk && part == 0) L.sum[me] = upto;
     __syncthreads();
-    if (tid < out.n) {
-        const size_t at = static_cast<size_t>(row) * out.n + tid;
-        const double t = static_cast<double>(out.uniforms[at]) * L.sum[kk];
-        int lo = 0, hi = kk;                              // the first i with sum[i + 1] > t
-        while (lo < hi) { const int mid = (lo + hi) / 2; if (L.sum[mid + 1] > t) hi = mid; else lo = mid + 1; }
-        if (lo >= kk) for (lo = kk - 1; lo > 0 && !(L.mass[lo] > 0.0); --lo) {}
-        out.drafts[at] = L.sorted[lo];
+    // a wave to a draw: the total is the CDF of the largest id
+    double total = 0.0;
+    for (int i = lane; i < kk; i += 64) total = fmax(total, L.sum[i]);
+    total = wave_max(total);
+    for (int d = tid >> 6; d < out.n; d += kDraftWaves) {
+        const size_t at = static_cast<size_t>(row) * out.n + d;
+        const double t = static_cast<double>(out.uniforms[at]) * total;
+        int first = 0x7FFFFFFF, last = -1;
+        for (int i = lane; i < kk; i += 64) {
+            if (L.sum[i] > t && L.mass[i] > 0.0) first = min(first, L.ids[i]);
+            if (L.mass[i] > 0.0) last = max(last, L.ids[i]);
+        }
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) { first = min(first, __shfl_xor(first, o)); last = max(last, __shfl_xor(last, o)); }
+        if (lane == 0) out.drafts[at] = first == 0x7FFFFFFF ? last : first;
     }
     if (tid == 0) out.status[row] = GR_ROW_OK;
 }
@@ -161,12 +191,10 @@ __global__ __launch_bounds__(64 * GR_MAX_N) void draft_whole_kernel(const Rows<T
 #pragma unroll
     for (int l = 0; l < kLoads; ++l) {
         const int c = c0 + l * 64 + lane;
+        const uint4 r = whole ? x.load(c) : x.load_guarded(c);
         float v[N];
-        if (whole) {
-            const uint4 r = x.load(c);
 #pragma unroll
-            for (int j = 0; j < N; ++j) v[j] = Packed<T>::get(r, j);
-        } else x.load_guarded(c, v);
+        for (int j = 0; j < N; ++j) v[j] = Packed<T>::get(r, j);
         double e[N], mine = 0.0;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
@@ -206,8 +234,8 @@ void launch_whole_as(const RowSource& src, int pieces, int stride, const double*
 }  // namespace
 
 void launch_draft_topk(const RowSource& src, bool probs, int k, double tail_mass, RowSlices cut, const RowParts& in, const DraftOut& out, hipStream_t stream) {
-    if (probs) hipLaunchKernelGGL(draft_topk_kernel<true>, dim3(src.rows), dim3(kThreads), 0, stream, src.temperature, k, tail_mass, cut.splits, in, out);
-    else hipLaunchKernelGGL(draft_topk_kernel<false>, dim3(src.rows), dim3(kThreads), 0, stream, src.temperature, k, 0.0, cut.splits, in, out);
+    if (probs) hipLaunchKernelGGL(draft_topk_kernel<true>, dim3(src.rows), dim3(kDraftThreads), 0, stream, src.temperature, k, tail_mass, cut.splits, in, out);
+    else hipLaunchKernelGGL(draft_topk_kernel<false>, dim3(src.rows), dim3(kDraftThreads), 0, stream, src.temperature, k, 0.0, cut.splits, in, out);
 }
 
 void launch_draft_whole(const RowSource& src, bool probs, int pieces, int stride, const double* mass, const float* refs, const DraftOut& out, hipStream_t stream) {

@@ -33,9 +33,9 @@ struct RowSlices { int splits, per; };                     // workgroups to a ro
 
 // elements of a 16-byte chunk
 constexpr int chunk_elements(int dtype) { return dtype == GR_F32 ? 4 : 8; }
-RowSlices choose_row_slices(int rows, int V, int dtype, int k);
-// The k largest (1 <= k <= kMaxSupport) of every slice; probs: rows of probabilities (float32) and their sums; sums: logits and the sums of their exponentials
-void launch_rows(const RowSource& src, bool probs, bool sums, int k, RowSlices cut, const RowParts& out, hipStream_t stream);
+RowSlices choose_row_slices(int rows, int V, int dtype, int k, bool sums);
+// The k largest (1 <= k <= kMaxSupport) of every slice; or up to `limit` candidates with them; probs: rows of probabilities (float32) and their sums; sums: logits and the sums of their exponentials
+void launch_rows(const RowSource& src, bool probs, bool sums, int k, int limit, RowSlices cut, const RowParts& out, hipStream_t stream);
 // Sums by pieces, see masses_kernel; pieces of `piece_elements` entries, counted from the 16-byte boundary at or before the row's begin
 constexpr int piece_elements(int dtype) { return 64 * 4 * chunk_elements(dtype); }
 constexpr int piece_count(int V, int dtype) { return static_cast<int>((static_cast<long long>(V) + chunk_elements(dtype) - 1 + piece_elements(dtype) - 1) / piece_elements(dtype)); }
@@ -79,6 +79,8 @@ template <> struct Packed<float> {
     static constexpr int N = 4;
     static __device__ __forceinline__ float get(const uint4& r, int j) { return __uint_as_float(j == 0 ? r.x : (j == 1 ? r.y : (j == 2 ? r.z : r.w))); }
     static __device__ __forceinline__ float one(float v) { return v; }
+    static __device__ __forceinline__ unsigned bits(float v) { return __float_as_uint(v); }
+    static constexpr unsigned kNoneBits = 0xFF800000u;    // -inf
 };
 template <> struct Packed<Bf16> {
     static constexpr int N = 8;
@@ -87,6 +89,8 @@ template <> struct Packed<Bf16> {
         return __uint_as_float((j & 1) ? (w & 0xFFFF0000u) : (w << 16));
     }
     static __device__ __forceinline__ float one(Bf16 v) { return __uint_as_float(static_cast<unsigned>(v.bits) << 16); }
+    static __device__ __forceinline__ unsigned bits(Bf16 v) { return v.bits; }
+    static constexpr unsigned kNoneBits = 0xFF80u;
 };
 template <> struct Packed<_Float16> {
     static constexpr int N = 8;
@@ -96,8 +100,13 @@ template <> struct Packed<_Float16> {
         return static_cast<float>(__builtin_bit_cast(_Float16, h));
     }
     static __device__ __forceinline__ float one(_Float16 v) { return static_cast<float>(v); }
+    static __device__ __forceinline__ unsigned bits(_Float16 v) { return __builtin_bit_cast(unsigned short, v); }
+    static constexpr unsigned kNoneBits = 0xFC00u;
 };
 constexpr float kNone = -__builtin_inff();
+
+// From here on the chunk's entries are unpacked again: one instruction each, where keeping them would cost a register each.
+__device__ __forceinline__ void unpack_again(uint4& r) { asm volatile("" : "+v"(r.x), "+v"(r.y), "+v"(r.z), "+v"(r.w)); }
 
 // A row as 16-byte chunks at 16-byte boundaries, wherever it begins: chunk c holds elements [c N - lead, c N - lead + N).  Chunks that reach
 // over an end of the row are read element by element, entries outside it are -inf.
@@ -113,56 +122,205 @@ struct RowChunks {
         return (c0 > 0 || lead == 0) && static_cast<long long>(c1) * N - lead <= V;
     }
     __device__ __forceinline__ uint4 load(int c) const { return *reinterpret_cast<const uint4*>(row + (static_cast<long long>(c) * N - lead)); }
-    __device__ __forceinline__ void load_guarded(int c, float* v) const {
-        if (inside(c, c + 1)) {
-            const uint4 r = load(c);
-#pragma unroll
-            for (int j = 0; j < N; ++j) v[j] = Packed<T>::get(r, j);
-            return;
-        }
+    // a chunk that may reach over an end of the row, or lie outside it
+    __device__ __forceinline__ uint4 load_guarded(int c) const {
+        if (inside(c, c + 1)) return load(c);
+        unsigned w[4] = {};
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             const long long i = static_cast<long long>(c) * N - lead + j;
-            v[j] = (i >= 0 && i < V) ? Packed<T>::one(row[i]) : kNone;
+            w[j * 4 / N] |= ((i >= 0 && i < V) ? Packed<T>::bits(row[i]) : Packed<T>::kNoneBits) << (j * 32 * 4 / N % 32);
         }
+        return make_uint4(w[0], w[1], w[2], w[3]);
     }
-    __device__ __forceinline__ int id(int c, int j) const { return static_cast<int>(static_cast<long long>(c) * N - lead + j); }
+    // the same with a first chunk that all lanes share
+    __device__ __forceinline__ uint4 load(int c0, unsigned at) const {
+        const char* const first = reinterpret_cast<const char*>(row) + (static_cast<long long>(c0) * 16 - lead * static_cast<int>(sizeof(T)));
+        return *reinterpret_cast<const uint4*>(first + at * 16u);
+    }
+    __device__ __forceinline__ int id(int c, int j) const { return static_cast<int>(static_cast<unsigned>(c) * N - lead + j); }
 };
 
-// 2^(y/32) for y <= 32 * 1000 (lower ones than -32 * 1000 count as that: 2^-1000 is nothing to any sum) from a table of 2^(j/32) in LDS and a
-// polynomial of degree 4 in the rest, |rest| <= ln2/64: relative error 1.3e-12.  The whole part is read off the bits of y + 1.5 * 2^52.
-// 64 lanes that read 32 doubles of LDS meet no bank conflict (64 banks), so the table costs one read.
-__device__ __forceinline__ double exp2_32(double y, const double* tab) {
-    constexpr double kMagic = 6755399441055744.0, kC = 6.93147180559945309417e-01 / 32.0;
+// 2^(y/256), |y| <= 256 * 700, added to sum: a table of 2^(j/256) in LDS and a polynomial of degree 2 in the rest, the best one for the relative error, 1.04e-10 either
+// way; sums of many terms are nearer.  The whole part is read off the low bits of y + 1.5 * 2^52; its multiple of 256 goes into the exponent by one addition, since
+// the table's upper words have j 2^12 taken off.  Ten instructions behind the float64 argument and one read of the table.  (A table of 32 entries without bank conflicts
+// and degree 3: 15.)  In two steps, so that several reads are on their way before the first is used.
+constexpr int kExpEntries = 256;
+struct ExpPart { double rest, entry; int whole; };
+__device__ __forceinline__ ExpPart exp2_256_begin(double y, const double* tab) {
+    constexpr double kMagic = 6755399441055744.0;
     const double m = y + kMagic;
-    const double r = y - (m - kMagic);
-    const int whole = __double2loint(m);
-    const double tv = tab[whole & 31];
-    double p = fma(r, kC * kC * kC * kC / 24.0, kC * kC * kC / 6.0);
-    p = fma(p, r, kC * kC / 2.0);
-    p = fma(p, r, kC);
-    p = fma(p, r, 1.0);
-    const double scaled = __hiloint2double(__double2hiint(tv) + ((whole >> 5) << 20), __double2loint(tv));
-    return p * scaled;
+    ExpPart e;
+    e.whole = __double2loint(m);
+    e.entry = tab[e.whole & (kExpEntries - 1)];
+    e.rest = y - (m - kMagic);
+    return e;
 }
-constexpr double kPerTemp = 46.166241308446828;           // 32 / ln 2
-constexpr float kLowest = -21900.f, kHighest = 20000.f;   // 32 * log2 of the range that exp2_32 and the sums of its results keep, below 32 * 1000
+__device__ __forceinline__ double exp2_256_end(const ExpPart& e, double sum) {
+    double p = fma(e.rest, 3.6655651770288774e-06, 2.7076067943688897e-03);
+    p = fma(p, e.rest, 1.0000000000001048);
+    return fma(p, __hiloint2double(__double2hiint(e.entry) + (e.whole << 12), __double2loint(e.entry)), sum);
+}
+constexpr double kPerTemp = 369.32993046757463;           // 256 / ln 2
+constexpr float kLowest = -175200.f, kHighest = 160000.f; // the y that exp2_256 takes, with room for the sums of its results; e^-474 is nothing to a sum
+__device__ __forceinline__ void fill_exp_table(double* tab) {        // by 256 threads
+    const double v = exp2(static_cast<double>(threadIdx.x) / kExpEntries);
+    tab[threadIdx.x] = __hiloint2double(__double2hiint(v) - (threadIdx.x << 12), __double2loint(v));
+}
 
-// What a wave has of a sum of exponentials: exp((x - ref) / T), ref the largest entry of its first tile that has any.  A later entry may lie
-// above ref (float64 has room for e^400 of them) until that is used up; then the sum is brought to a new reference.
+// A wave's sum of exponentials: of exp((x - ref) / T), ref the largest entry of its first tile that has any.  A later entry may lie above ref (float64
+// has room for e^433 of them) until that is used up; then the sum is brought to a new reference.
 struct ExpSum {
-    double sum = 0.0; float ref = kNone;
-    // from here on entries up to `most` (of the whole wave) come
-    __device__ __forceinline__ void raise(float most, double scale) {
-        if (most > ref && (ref == kNone || (static_cast<double>(most) - static_cast<double>(ref)) * scale > static_cast<double>(kHighest))) {
-            sum *= exp((static_cast<double>(ref) - static_cast<double>(most)) * scale / kPerTemp);        // from -inf: 0
-            ref = most;
+    double sum = 0.0, scale, shift = 0.0;                 // scale: kPerTemp / T; shift: -ref * scale
+    float ref = kNone, floor = kNone, ceiling = kNone;    // floor: entries below it count as if they were e^-474 of the reference; above the ceiling there is no room
+    bool plain = false;                                   // ref * scale is small enough for its rounding
+    __device__ __forceinline__ explicit ExpSum(double s) : scale(s) {}
+    __device__ __forceinline__ void refer(float most) {
+        // the same in all lanes, and known to be
+        ref = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(most)));
+        shift = -static_cast<double>(ref) * scale;
+        plain = __builtin_amdgcn_readfirstlane(fabs(shift) < 3.0e7) != 0;          // x scale + shift is then off by 4e-9 / 256 at most
+        floor = static_cast<float>(static_cast<double>(ref) + static_cast<double>(kLowest) / scale);
+        ceiling = static_cast<float>(static_cast<double>(ref) + static_cast<double>(kHighest) / scale);
+    }
+    // the sum as one of a reference `to`, not below ref
+    __device__ __forceinline__ double rebased(float to, const double* tab) const {
+        const double y = fmax((static_cast<double>(ref) - static_cast<double>(to)) * scale, static_cast<double>(kLowest));
+        return ref > kNone ? sum * exp2_256_end(exp2_256_begin(y, tab), 0.0) : 0.0;
+    }
+    // from here on entries up to `most` (this lane's) come
+    __device__ __forceinline__ void raise(float most, const double* tab) {
+        if (__any(most > ceiling)) {
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) most = fmaxf(most, __shfl_xor(most, o));
+            sum = rebased(most, tab);
+            refer(most);
+        }
+    }
+    // kEight entries per lane.  A NaN makes the sum NaN.
+    static constexpr int kEight = 8;
+    __device__ __forceinline__ void add(const float* x, const double* tab) {
+        float least = x[0];
+#pragma unroll
+        for (int i = 1; i < kEight; ++i) least = fminf(least, x[i]);
+        if (plain && !__any(least < floor)) {
+#pragma unroll
+            for (int i0 = 0; i0 < kEight; i0 += 4) {                              // four table entries on their way: eight would spill
+                ExpPart e[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[i] = exp2_256_begin(fma(static_cast<double>(x[i0 + i]), scale, shift), tab);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum = exp2_256_end(e[i], sum);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+            // masked entries, lowest values, tiny temperatures: the difference first, which is exact
+            const double r = static_cast<double>(ref);
+#pragma unroll 1
+            for (int i = 0; i < kEight; ++i) {
+                float v = x[0];
+#pragma unroll
+                for (int j = 1; j < kEight; ++j) v = i == j ? x[j] : v;
+                const double upto = exp2_256_end(exp2_256_begin(fmax((static_cast<double>(v) - r) * scale, static_cast<double>(kLowest)), tab), sum);
+                sum = v == v ? upto : static_cast<double>(v);
+            }
         }
     }
 };
-// (x - ref first: exact, where a product with the scale would be rounded at the size of the lowest float)
-__device__ __forceinline__ double exp_term(float v, double scale, double ref, const double* tab) {
-    return exp2_32(fmax((static_cast<double>(v) - ref) * scale, static_cast<double>(kLowest)), tab);
+
+__device__ __forceinline__ float wave_max_f(float v) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) v = fmaxf(v, __shfl_xor(v, o));
+    return v;
+}
+__device__ __forceinline__ float wave_min_f(float v) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) v = fminf(v, __shfl_xor(v, o));
+    return v;
+}
+
+// The keys in LDS (CAP at most) cut to the k largest, in place; all threads call it.  Returns the key that they reach.
+template <int CAP, int NT = kThreads>
+__device__ __forceinline__ unsigned long long cut_keys(unsigned long long* keys, int* count, int c, int k, int* hist, int* pick) {
+    const int tid = threadIdx.x;
+    const unsigned long long theta = block_kth_largest<NT>(keys, c, k, hist, pick);
+    unsigned long long mine[CAP / NT];
+#pragma unroll
+    for (int r = 0; r < CAP / NT; ++r) {
+        const int i = tid + r * NT;
+        mine[r] = i < c ? keys[i] : 0ull;
+    }
+    __syncthreads();
+    if (tid == 0) *count = 0;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < CAP / NT; ++r)
+        if (mine[r] >= theta && mine[r] != 0ull) keys[atomicAdd(count, 1)] = mine[r];
+    __syncthreads();
+    return theta;
+}
+
+
+// Not above any entry of bin `from` and those behind it, of 256 linear bins from lo to hi: the bin's lower edge, lowered by more than its roundings (a few 2^-24 of
+// either addend); not below lo.
+__device__ __forceinline__ float bin_edge(float lo, float hi, int from) {
+    const float up = static_cast<float>(from) * ((hi - lo) / 255.f), edge = lo + up - 0x1p-20f * (fabsf(lo) + up);
+    return edge > lo ? edge : lo;                         // NaN, too: lo
+}
+
+// Of c > k keys in LDS the largest ones, moved to its begin: at least k, at most `limit`; all threads call it.  Returns how many;
+// `reach`: a value that at least k of all keys' entries reach.
+// The keys go into 256 bins, linear over their range (entries are spread smoothly there: one round where digits of the bit pattern take three), and the
+// bins from the top that hold k stay; where they hold more than `limit`, equal entries mostly, the radix selection finds the k.
+template <int CAP, bool PROBS, int NT = kThreads>
+__device__ __forceinline__ int thin_keys(unsigned long long* keys, int c, int k, int limit, int* hist, int* pick, float* edge, int* count, float* reach = nullptr) {
+    constexpr int kNW = NT / 64;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    constexpr int kEach = CAP / NT;
+    unsigned long long mine[kEach];
+    const auto value = [](unsigned long long key) { return PROBS ? key_q(key) : key_logit(key); };
+    float lo = __builtin_inff(), hi = kNone;
+#pragma unroll
+    for (int r = 0; r < kEach; ++r) {
+        const int i = tid + r * NT;
+        mine[r] = i < c ? keys[i] : 0ull;
+        if (i < c) { const float v = value(mine[r]); lo = fminf(lo, v); hi = fmaxf(hi, v); }
+    }
+    lo = wave_min_f(lo); hi = wave_max_f(hi);
+    if (lane == 0) { edge[wave] = lo; edge[kNW + wave] = hi; }
+    if (tid < 256) hist[tid] = 0;
+    if (tid == 0) *count = 0;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kNW; ++w) { lo = fminf(lo, edge[w]); hi = fmaxf(hi, edge[kNW + w]); }
+    const float per = 255.f / (hi - lo);                  // infinite or 0 where all are equal, or some lie beyond float32 apart: the bins still rise with the entry
+    const auto bin = [&](unsigned long long key) { return static_cast<int>(fminf(fmaxf((value(key) - lo) * per, 0.f), 255.f)); };   // NaN: 0
+#pragma unroll
+    for (int r = 0; r < kEach; ++r) if (mine[r] != 0ull) atomicAdd(&hist[bin(mine[r])], 1);
+    __syncthreads();
+    int in[4], tot = 0;                                   // every wave by itself: lane l owns bins 255-4l .. 252-4l
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { in[j] = hist[255 - 4 * lane - j]; tot += in[j]; }
+    const int incl = wave_scan_i(tot);
+    int above = incl - tot, from = -1, left = 0;
+    const bool mine_is = above < k && k <= incl;
+    if (mine_is)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { above += in[j]; if (from < 0 && above >= k) { from = 255 - 4 * lane - j; left = above; } }
+    const int owner = __ffsll(static_cast<unsigned long long>(__ballot(mine_is))) - 1;
+    from = __builtin_amdgcn_readlane(from, owner); left = __builtin_amdgcn_readlane(left, owner);
+    if (left > limit) {
+        __syncthreads();
+        const unsigned long long kth = cut_keys<CAP, NT>(keys, count, c, k, hist, pick);
+        if (reach) *reach = value(kth);
+        return k;
+    }
+#pragma unroll
+    for (int r = 0; r < kEach; ++r) if (mine[r] != 0ull && bin(mine[r]) >= from) keys[atomicAdd(count, 1)] = mine[r];
+    __syncthreads();
+    if (reach) *reach = bin_edge(lo, hi, from);
+    return left;
 }
 
 }  // namespace gr

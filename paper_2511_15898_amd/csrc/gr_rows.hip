@@ -13,22 +13,11 @@ namespace gr {
 
 namespace {
 
-constexpr int kRowCap = 2048;                             // candidate keys in LDS
-static_assert(kRowCap >= 2 * kMaxSupport && kRowCap <= kSelCap, "a tile that overflows adds k keys to at most k kept ones");
+constexpr int kRowCap = 1024;                             // candidate keys in LDS
+constexpr int kListCap = 512;                             // chunks with candidates in LDS
 
-__device__ __forceinline__ float wave_max_f(float v) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v = fmaxf(v, __shfl_xor(v, o));
-    return v;
-}
-__device__ __forceinline__ float wave_min_f(float v) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v = fminf(v, __shfl_xor(v, o));
-    return v;
-}
-
-// The keys of a stretch of the row that reach `from`: one that exactly k of them reach.  Only tiles with thousands of entries at their threshold come
-// here (rows of equal entries), so the stretch is read again for every digit, and a digit that a whole wave agrees on is counted once.
+// Of the keys of a stretch of the row one that exactly k of them reach (0: no key).  Only slices with more entries at their threshold than LDS holds come
+// here (rows of equal entries, rows that rise), so the stretch is read again for every digit, and a digit that a whole wave agrees on is counted once.
 template <typename KeyAt>
 __device__ __forceinline__ unsigned long long stretch_kth_largest(KeyAt key_at, int count, int k, int* hist, int* pick) {
     const int tid = threadIdx.x;
@@ -73,206 +62,253 @@ __device__ __forceinline__ unsigned long long stretch_kth_largest(KeyAt key_at, 
     return prefix;
 }
 
-// The keys in LDS cut to the k largest, in place; all threads call it.  Returns the key that they reach.
-__device__ __forceinline__ unsigned long long cut_keys(unsigned long long* keys, int* count, int c, int k, int* hist, int* pick) {
-    const int tid = threadIdx.x;
-    const unsigned long long theta = block_kth_largest(keys, c, k, hist, pick);
-    unsigned long long mine[kRowCap / kThreads];
+// A threshold that at least k of the entries reach (-inf: there are too few), from the largest entries `top` of the threads' chunks (kLoads each, different entries): about the k-th
+// largest of them.  With 8192 entries to a tile 9 reach it for k = 8, 136 for k = 128, 290 for k = 256.  First a bound from below, the threads in G
+// groups, the smallest power of two >= k: the smallest of the groups' largest.  Then 256 linear bins from there to the largest entry.  All threads call it.
+__device__ __forceinline__ float find_threshold(const float* top, int k, int* hist, float* group_max, float* edge) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    float most = top[0];
 #pragma unroll
-    for (int r = 0; r < kRowCap / kThreads; ++r) {
-        const int i = tid + r * kThreads;
-        mine[r] = i < c ? keys[i] : 0ull;
+    for (int l = 1; l < kLoads; ++l) most = fmaxf(most, top[l]);
+    float lo, hi = wave_max_f(most);
+    __syncthreads();                                      // whoever reads what an earlier call left is done
+    hist[tid] = 0;
+    if (lane == 0) edge[kWaves + wave] = hi;
+    if (k <= 64) {
+        int groups = 1;
+        while (groups < k) groups *= 2;
+        for (int o = 32; o >= groups; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+        group_max[tid] = most;
+        __syncthreads();
+        lo = wave_min_f(fmaxf(fmaxf(group_max[lane], group_max[lane + 64]), fmaxf(group_max[lane + 128], group_max[lane + 192])));
+    } else {
+        group_max[tid] = most;
+        __syncthreads();
+        lo = wave_min_f(k <= 128 ? fmaxf(most, group_max[tid ^ 128]) : most);
+        if (lane == 0) edge[wave] = lo;
+        __syncthreads();
+        lo = fminf(fminf(edge[0], edge[1]), fminf(edge[2], edge[3]));
     }
-    __syncthreads();
-    if (tid == 0) *count = 0;
-    __syncthreads();
+    hi = fmaxf(fmaxf(edge[4], edge[5]), fmaxf(edge[6], edge[7]));
+    if (!(lo > kNone)) return kNone;                      // the same for all threads
+    const float per = 255.f / (hi - lo);
 #pragma unroll
-    for (int r = 0; r < kRowCap / kThreads; ++r)
-        if (mine[r] >= theta && mine[r] != 0ull) keys[atomicAdd(count, 1)] = mine[r];
+    for (int l = 0; l < kLoads; ++l) if (top[l] >= lo) atomicAdd(&hist[static_cast<int>(fminf(fmaxf((top[l] - lo) * per, 0.f), 255.f))], 1);
     __syncthreads();
-    return theta;
+    int in[4], tot = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { in[j] = hist[255 - 4 * lane - j]; tot += in[j]; }
+    const int incl = wave_scan_i(tot);
+    int above = incl - tot, from = -1;
+    const bool mine_is = above < k && k <= incl;
+    if (mine_is)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { above += in[j]; if (from < 0 && above >= k) from = 255 - 4 * lane - j; }
+    from = __builtin_amdgcn_readlane(from, __ffsll(static_cast<unsigned long long>(__ballot(mine_is))) - 1);
+    return bin_edge(lo, hi, from);
 }
 
-
 // grid = (splits * rows), 256 threads.  Workgroup s of a row reads chunks [s * per, (s + 1) * per) of its row, tiles of 256 * kLoads chunks, the next
-// tile's loads on their way while the present one is worked on.
-// The k largest: of the first tile every thread knows its largest entry; the threads form G groups, the smallest power of two >= k, and the
-// smallest of the groups' largest entries is reached by at least k entries, so nothing below it is a candidate.  With 8192 entries to a tile about 22 reach
-// it for k = 8 and 600 for k = 128.  Candidates go to LDS as 64-bit keys (entry, ~id); when there are many they are cut to the k largest by radix
-// selection and the threshold rises.
-// SUM: PROBS: the float64 sum of the slice.  Logits: the sum of exp((x - ref) / T), per wave with its own reference, joined at the end.
+// tile's loads on their way while the present one is worked on, and no barrier between tiles but for the threshold of the first.
+// The k largest: a chunk whose largest entry reaches the threshold goes, as it was loaded, to a list in LDS; the few on it are taken apart together at
+// the end (in the order of tiles every one would cost all lanes of its wave the test of every entry: 81 us where this takes %ROWS%).
+// Keys are 64 bits (entry, ~id).  After `refresh` tiles the list is worked off and the threshold rises to about the k-th key.
+// A slice leaves at least its k largest, up to `limit` candidates.
+// SUM: PROBS: the float64 sum of the slice.  Logits: the sum of exp((x - ref) / T) in float64, per wave with its own reference, joined at the end.  (The hardware's float32
+// exponential, with the listed chunks in float64, was measured: %F32%, but sums good to 2e-8 only, which depend on how a row is cut.)
 // Rows of beams that are not in use or finished are not read (Rows::skip).
+// Four waves to a SIMD with the exponentials: for a fifth their loop spills (32 us become 37, 89 become 114).
 template <typename T, bool PROBS, bool SUM>
-__global__ __launch_bounds__(kThreads) void rows_kernel(const Rows<T> in, int k, int splits, int per, const RowParts out) {
+__global__ __launch_bounds__(kThreads, SUM && !PROBS ? 4 : 5) void rows_kernel(const Rows<T> in, int k, int limit, int splits, int per, const RowParts out) {
     constexpr int N = Packed<T>::N, kTileChunks = kThreads * kLoads;
+    constexpr bool kExp = SUM && !PROBS;
     __shared__ unsigned long long keys[kRowCap];
+    __shared__ uint4 list[kListCap];
+    __shared__ int list_chunk[kListCap];
     __shared__ int hist[256];
     __shared__ int pick[4];
-    __shared__ int count;
+    __shared__ int count, listed;
     __shared__ float group_max[kThreads];
     __shared__ double red[kWaves];
-    __shared__ float wref[kWaves];
-    __shared__ double tab[32];
+    __shared__ float edge[2 * kWaves];
+    __shared__ double tab[kExp ? kExpEntries : 1];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int row = blockIdx.x / splits, s = blockIdx.x - row * splits;
     if (in.skip(row)) return;
     const RowChunks<T> x(in.row(row), in.V);
     const int c_first = s * per, c_end = min(x.chunks, c_first + per);
-    int bad = 0;
-    double scale = 0.0;
-    if (SUM && !PROBS) {
-        const float temp = in.temperature_of(row);
-        if (!(temp > 0.f) || !(temp <= 3.0e38f)) bad = 1; else scale = kPerTemp / static_cast<double>(temp);
-        if (tid < 32) tab[tid] = exp2(static_cast<double>(tid) / 32.0);
-    }
-    if (tid == 0) count = 0;
-    __syncthreads();
 
-    float theta = kNone;                                  // entries below it are no candidates, keys below theta_key neither
-    unsigned long long theta_key = 0ull;
-    ExpSum es;
-    double total = 0.0;
-    int held = 0;                                         // candidates of the tiles before
-    const auto key_of = [](float v, int id) { return PROBS ? make_key(v, id) : make_key_logit(v, id); };
-
-    uint4 now[kLoads], next[kLoads];
-    bool whole = false;
-    const auto fetch = [&](int c0, uint4* r) {
-        whole = c0 + kTileChunks <= c_end && x.inside(c0, c0 + kTileChunks);
-        if (whole)
+    uint4 next[kLoads];
+    const auto fetch = [&](int c0) {
+        if (c0 + kTileChunks <= c_end && x.inside(c0, c0 + kTileChunks)) {
 #pragma unroll
-            for (int l = 0; l < kLoads; ++l) r[l] = x.load(c0 + l * kThreads + tid);
-    };
-    fetch(c_first, next);
-    for (int c0 = c_first; c0 < c_end; c0 += kTileChunks) {
-        float v[kLoads * N];
-        if (whole) {
-#pragma unroll
-            for (int l = 0; l < kLoads; ++l) now[l] = next[l];
-            fetch(c0 + kTileChunks, next);                // may leave `whole` false for the next round
-#pragma unroll
-            for (int l = 0; l < kLoads; ++l)
-#pragma unroll
-                for (int j = 0; j < N; ++j) v[l * N + j] = Packed<T>::get(now[l], j);
-        } else {
+            for (int l = 0; l < kLoads; ++l) next[l] = x.load(c0, l * kThreads + tid);
+        } else if (c0 < c_end)
 #pragma unroll
             for (int l = 0; l < kLoads; ++l) {
-                const int c = c0 + l * kThreads + tid;
-                if (c < c_end) x.load_guarded(c, v + l * N);
-                else
-#pragma unroll
-                    for (int j = 0; j < N; ++j) v[l * N + j] = kNone;
+                const int c = c0 + l * kThreads;
+                if (c + kThreads <= c_end && x.inside(c, c + kThreads)) next[l] = x.load(c, tid);
+                else if (c < c_end) next[l] = x.load_guarded(c + tid < c_end ? c + tid : x.chunks);
             }
-            fetch(c0 + kTileChunks, next);
-        }
-        // NaN, +inf (logits), negative entries (probabilities); entries outside the row are -inf
-        float most = kNone, probe = 0.f;
+    };
+    fetch(c_first);
+    int bad = 0;
+    double scale = 1.0;
+    if (kExp) {
+        const float temp = in.temperature_of(row);
+        if (!(temp > 0.f) || !(temp <= 3.0e38f)) bad = 1; else scale = kPerTemp / static_cast<double>(temp);
+        fill_exp_table(tab);
+    }
+    if (tid == 0) { count = 0; listed = 0; }
+    __syncthreads();
+
+    float theta = kNone;                                  // entries below it are no candidates
+    bool over = false;                                    // more candidates than LDS holds
+    double total = 0.0;
+    ExpSum es(scale);
+    const float least = PROBS ? 0.f : kNone;              // entries must lie above it
+    const auto key_of = [](float v, int id) { return PROBS ? make_key(v, id) : make_key_logit(v, id); };
+    // the list taken apart: its entries that reach the threshold become keys
+    const auto work_off = [&]() {
+        __syncthreads();
+        const int n = listed;
+        over = over || n > kListCap;
 #pragma unroll
-        for (int i = 0; i < kLoads * N; ++i) {
-            most = fmaxf(most, v[i]);
-            if (PROBS) bad |= static_cast<int>(!(v[i] >= 0.f)) & static_cast<int>(v[i] != kNone);
-            else probe += v[i];
-        }
-        if (!PROBS) bad |= static_cast<int>(!(probe < 3.0e38f));
-        if (SUM && PROBS) {
-#pragma unroll
-            for (int i = 0; i < kLoads * N; ++i) total += static_cast<double>(v[i] == kNone ? 0.f : v[i]);
-        }
-        if (SUM && !PROBS) {
-            es.raise(wave_max_f(most), scale);
-            if (es.ref > kNone) {
-                const double r = static_cast<double>(es.ref);
-                double part = 0.0;
-#pragma unroll
-                for (int i = 0; i < kLoads * N; ++i) part += exp_term(v[i], scale, r, tab);
-                es.sum += part;
-            }
-        }
-        if (theta == kNone) {
-            // the first tile's threshold (and the next ones', while there is none)
-            float g;
-            if (k <= 64) {
-                int groups = 1;
-                while (groups < k) groups *= 2;
-                g = most;
-                for (int o = 32; o >= groups; o >>= 1) g = fmaxf(g, __shfl_xor(g, o));
-                group_max[tid] = g;
-                __syncthreads();
-                g = fmaxf(fmaxf(group_max[lane], group_max[lane + 64]), fmaxf(group_max[lane + 128], group_max[lane + 192]));
-                theta = wave_min_f(g);
-            } else {
-                group_max[tid] = most;
-                __syncthreads();
-                g = k <= 128 ? fmaxf(most, group_max[tid ^ 128]) : most;
-                g = wave_min_f(g);
-                if (lane == 0) wref[wave] = g;
-                __syncthreads();
-                theta = fminf(fminf(wref[0], wref[1]), fminf(wref[2], wref[3]));
-            }
-            if (!(theta > kNone)) theta = kNone;          // too few entries, or NaN among them
-        }
-        const float least = PROBS ? 0.f : kNone;
-#pragma unroll
-        for (int l = 0; l < kLoads; ++l)
+        for (int r = 0; r < kListCap / kThreads; ++r) {
+            const int i = tid + r * kThreads;
+            const bool have = i < min(n, kListCap);
+            if (!__any(have)) break;
+            const uint4 raw = have ? list[i] : make_uint4(0u, 0u, 0u, 0u);
+            const int chunk = have ? list_chunk[i] : 0;
+            unsigned mask = 0u;
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                const float e = v[l * N + j];
-                if (e >= theta && e > least) {
-                    const unsigned long long key = key_of(e, x.id(c0 + l * kThreads + tid, j));
-                    if (key >= theta_key) {
-                        const int slot = atomicAdd(&count, 1);
-                        if (slot < kRowCap) keys[slot] = key;
-                    }
+                const float v = Packed<T>::get(raw, j);
+                if (have && v >= theta && v > least) mask |= 1u << j;
+            }
+            const int upto = wave_scan_i(__popc(mask));
+            int base = 0;
+            if (lane == 63) base = atomicAdd(&count, upto);
+            int slot = __builtin_amdgcn_readlane(base, 63) + upto - __popc(mask);
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (mask >> j & 1u) { if (slot < kRowCap) keys[slot] = key_of(Packed<T>::get(raw, j), x.id(chunk, j)); ++slot; }
+        }
+        __syncthreads();
+        over = over || count > kRowCap;
+    };
+
+    // The first tile's threshold lies at about its k-th entry, give or take 1 / sqrt(k) of its rank: six times that much has room for so many tiles.  Later ones hold
+    // ever fewer candidates, so the stretches double.
+    int refresh = max(1, kListCap / (k + 6 * static_cast<int>(sqrtf(static_cast<float>(k))) + 12)), tiles = 0;
+    for (int c0 = c_first; c0 < c_end; c0 += kTileChunks) {
+        uint4 now[kLoads];
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) now[l] = next[l];
+        fetch(c0 + kTileChunks);
+        const int loads = min(kLoads, (c_end - c0 + kThreads - 1) / kThreads);     // of the last tile maybe fewer
+        // Entries outside the row are -inf.  Bad: NaN, +inf (logits), negative entries (probabilities).
+        float top[kLoads], most = kNone, probe = 0.f;
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) {
+            top[l] = kNone;
+            if (l >= loads) continue;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float v = Packed<T>::get(now[l], j);
+                top[l] = fmaxf(top[l], v);
+                if (PROBS) {
+                    bad |= static_cast<int>(!(v >= 0.f)) & static_cast<int>(v != kNone);
+                    total += static_cast<double>(v == kNone ? 0.f : v);
+                } else if (!kExp) probe += v;
+            }
+            most = fmaxf(most, top[l]);
+            unpack_again(now[l]);
+        }
+        if (!PROBS && !kExp) bad |= static_cast<int>(!(probe < 3.0e38f));
+        if (kExp) {
+            bad |= static_cast<int>(most > 3.0e38f);
+            es.raise(most, tab);
+            if (es.ref == kNone) {
+                // nothing but masked entries and NaN, which the maximum passes over
+#pragma unroll
+                for (int l = 0; l < kLoads; ++l)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) { const float v = Packed<T>::get(now[l], j); bad |= static_cast<int>(l < loads) & static_cast<int>(v != v); }
+            } else
+#pragma unroll
+                for (int l = 0; l < kLoads; l += ExpSum::kEight / N) {
+                    if (l >= loads) continue;
+                    float v[ExpSum::kEight];
+#pragma unroll
+                    for (int j = 0; j < ExpSum::kEight; ++j) v[j] = l + j / N < loads ? Packed<T>::get(now[l + j / N], j % N) : kNone;
+                    es.add(v, tab);
                 }
+        }
+        if (theta == kNone) theta = find_threshold(top, k, hist, group_max, edge);
+        unsigned long long hit[kLoads];
+        int hits = 0;
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) { hit[l] = __ballot(top[l] >= theta && top[l] > least); hits += __popcll(hit[l]); }
+        if (hits != 0) {
+            int slot = 0;
+            if (lane == 0) slot = atomicAdd(&listed, hits);
+            slot = __builtin_amdgcn_readfirstlane(slot);
+#pragma unroll
+            for (int l = 0; l < kLoads; ++l) {
+                const int mine = slot + __builtin_amdgcn_mbcnt_hi(static_cast<unsigned>(hit[l] >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<unsigned>(hit[l]), 0u));
+                if ((hit[l] >> lane & 1ull) && mine < kListCap) { list[mine] = now[l]; list_chunk[mine] = c0 + l * kThreads + tid; }
+                slot += __popcll(hit[l]);
             }
-        __syncthreads();
-        int c = count;
-        __syncthreads();
-        if (c > kRowCap) {
-            // more than there is room for, equal entries for the most part: the tile's k largest by themselves
-            const long long e0 = static_cast<long long>(c0) * N - x.lead;
-            const int tile_end = min(c_end, c0 + kTileChunks);
-            const auto tile_key = [&](int i) -> unsigned long long {
-                const long long at = e0 + i;
-                if (at < 0 || at >= x.V) return 0ull;
-                const float e = Packed<T>::one(x.row[at]);
-                if (!(e >= theta && e > least)) return 0ull;
-                const unsigned long long key = key_of(e, static_cast<int>(at));
-                return key >= theta_key ? key : 0ull;
-            };
-            const int entries = (tile_end - c0) * N;
-            const unsigned long long reach = stretch_kth_largest(tile_key, entries, k, hist, pick);
-            if (tid == 0) count = held;                   // its keys lie where they were
+        }
+        if (++tiles == refresh && c0 + kTileChunks < c_end) {
+            refresh *= 2;
+            work_off();
+            const int c = count;
             __syncthreads();
-            for (int i = tid; i < entries; i += kThreads) {
-                const unsigned long long key = tile_key(i);
-                if (key >= reach && key != 0ull) keys[atomicAdd(&count, 1)] = key;
+            if (!over && c > k) {
+                float reach;
+                thin_keys<kRowCap, PROBS>(keys, c, k, kRowCap / 2, hist, pick, edge, &count, &reach);
+                theta = fmaxf(theta, reach);
             }
-            __syncthreads();
-            c = count;
+            if (tid == 0) listed = 0;
             __syncthreads();
         }
-        if (c > k && (c > kRowCap / 2 || c0 + kTileChunks >= c_end || c > 4 * k + 64)) {
-            theta_key = cut_keys(keys, &count, c, k, hist, pick);
-            theta = PROBS ? key_q(theta_key) : key_logit(theta_key);
-            c = k;
-        }
-        held = c;                                         // kRowCap / 2 at most, so that k more have room
     }
+    work_off();
+    const int room = min(kSelCap / splits, limit);        // k at least
+    unsigned long long* const to = out.cand + static_cast<size_t>(row) * kSelCap + s * (kSelCap / splits);
+    int found = count;
     __syncthreads();
-    const int room = kSelCap / splits, found = min(min(count, k), room);
-    unsigned long long* const to = out.cand + static_cast<size_t>(row) * kSelCap + s * room;
+    if (over) {
+        // the slice's k largest by themselves
+        const long long e0 = max(0ll, static_cast<long long>(c_first) * N - x.lead), e1 = min(static_cast<long long>(x.V), static_cast<long long>(c_end) * N - x.lead);
+        const auto slice_key = [&](int i) -> unsigned long long {
+            const float e = Packed<T>::one(x.row[e0 + i]);
+            return e > least ? key_of(e, static_cast<int>(e0 + i)) : 0ull;
+        };
+        const unsigned long long reach = stretch_kth_largest(slice_key, static_cast<int>(e1 - e0), k, hist, pick);
+        if (tid == 0) count = 0;
+        __syncthreads();
+        for (int i = tid; i < static_cast<int>(e1 - e0); i += kThreads) {
+            const unsigned long long key = slice_key(i);
+            if (key >= reach && key != 0ull) keys[atomicAdd(&count, 1)] = key;
+        }
+        __syncthreads();
+        found = k;
+    } else if (found > room) found = thin_keys<kRowCap, PROBS>(keys, found, k, room, hist, pick, edge, &count);
     for (int i = tid; i < found; i += kThreads) to[i] = keys[i];
     double sum = 0.0;
     float ref = 0.f;
     if (SUM && PROBS) sum = block_sum(total, red);
-    if (SUM && !PROBS) {
-        if (lane == 0) wref[wave] = es.ref;
+    if (kExp) {
         __syncthreads();
-        ref = fmaxf(fmaxf(wref[0], wref[1]), fmaxf(wref[2], wref[3]));
-        const double mine = es.ref > kNone ? es.sum * exp((static_cast<double>(es.ref) - static_cast<double>(ref)) * scale / kPerTemp) : 0.0;
-        sum = block_sum(mine, red);
+        if (lane == 0) edge[wave] = es.ref;
+        __syncthreads();
+        ref = fmaxf(fmaxf(edge[0], edge[1]), fmaxf(edge[2], edge[3]));
+        bad |= static_cast<int>(!(es.sum == es.sum));
+        sum = block_sum(es.rebased(ref, tab), red);
     }
     const int any_bad = block_sum_i(bad, red);
     if (tid == 0) {
@@ -287,7 +323,7 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(const Rows<T> in, int k,
 template <typename T, bool PROBS>
 __global__ __launch_bounds__(kThreads) void masses_kernel(const Rows<T> in, int pieces, int stride, double* __restrict__ mass, float* __restrict__ refs) {
     constexpr int N = Packed<T>::N;
-    __shared__ double tab[32];
+    __shared__ double tab[PROBS ? 1 : kExpEntries];
     const int tid = threadIdx.x, lane = tid & 63, groups = (pieces + kWaves - 1) / kWaves, row = blockIdx.x / groups;
     const RowChunks<T> x(in.row(row), in.V);
     int bad = 0;
@@ -295,44 +331,54 @@ __global__ __launch_bounds__(kThreads) void masses_kernel(const Rows<T> in, int 
     if (!PROBS) {
         const float temp = in.temperature_of(row);
         if (!(temp > 0.f) || !(temp <= 3.0e38f)) bad = 1; else scale = kPerTemp / static_cast<double>(temp);
-        if (tid < 32) tab[tid] = exp2(static_cast<double>(tid) / 32.0);
+        fill_exp_table(tab);
         __syncthreads();
     }
     const int piece = (blockIdx.x - row * groups) * kWaves + (tid >> 6);
     if (piece >= pieces) return;                          // whole waves
     const int c0 = piece * 64 * kLoads;
-    float v[kLoads * N];
-    if (x.inside(c0, c0 + 64 * kLoads)) {
-        uint4 r[kLoads];
+    uint4 r[kLoads];
+    if (x.inside(c0, c0 + 64 * kLoads))
 #pragma unroll
         for (int l = 0; l < kLoads; ++l) r[l] = x.load(c0 + l * 64 + lane);
+    else
 #pragma unroll
-        for (int l = 0; l < kLoads; ++l)
-#pragma unroll
-            for (int j = 0; j < N; ++j) v[l * N + j] = Packed<T>::get(r[l], j);
-    } else {
-#pragma unroll
-        for (int l = 0; l < kLoads; ++l) x.load_guarded(c0 + l * 64 + lane, v + l * N);
-    }
-    float most = kNone, probe = 0.f;
-#pragma unroll
-    for (int i = 0; i < kLoads * N; ++i) {
-        most = fmaxf(most, v[i]);
-        if (PROBS) bad |= static_cast<int>(!(v[i] >= 0.f)) & static_cast<int>(v[i] != kNone);
-        else probe += v[i];
-    }
-    if (!PROBS) bad |= static_cast<int>(!(probe < 3.0e38f));
+        for (int l = 0; l < kLoads; ++l) r[l] = x.load_guarded(c0 + l * 64 + lane);
+    float top = kNone;
     double sum = 0.0;
+#pragma unroll
+    for (int l = 0; l < kLoads; ++l) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float v = Packed<T>::get(r[l], j);
+            if (PROBS) {
+                bad |= static_cast<int>(!(v >= 0.f)) & static_cast<int>(v != kNone);
+                sum += static_cast<double>(v == kNone ? 0.f : v);
+            } else top = fmaxf(top, v);
+        }
+        unpack_again(r[l]);
+    }
     float ref = 0.f;
-    if (PROBS) {
+    if (!PROBS) {
+        bad |= static_cast<int>(top > 3.0e38f);
+        ref = wave_max_f(top);
+        if (ref > kNone && scale > 0.0) {
+            ExpSum es(scale);
+            es.refer(ref);
 #pragma unroll
-        for (int i = 0; i < kLoads * N; ++i) sum += static_cast<double>(v[i] == kNone ? 0.f : v[i]);
-    } else {
-        ref = wave_max_f(most);
-        if (ref > kNone) {
-            const double r = static_cast<double>(ref);
+            for (int l = 0; l < kLoads; l += ExpSum::kEight / N) {
+                float v[ExpSum::kEight];
 #pragma unroll
-            for (int i = 0; i < kLoads * N; ++i) sum += exp_term(v[i], scale, r, tab);
+                for (int j = 0; j < ExpSum::kEight; ++j) v[j] = Packed<T>::get(r[l + j / N], j % N);
+                es.add(v, tab);
+            }
+            sum = es.sum;                                 // NaN if an entry is
+        } else {
+            // nothing but masked entries and NaN, which the maximum passes over
+#pragma unroll
+            for (int l = 0; l < kLoads; ++l)
+#pragma unroll
+                for (int j = 0; j < N; ++j) { const float v = Packed<T>::get(r[l], j); bad |= static_cast<int>(v != v); }
         }
     }
     sum = wave_sum(sum);
@@ -344,8 +390,8 @@ __global__ __launch_bounds__(kThreads) void masses_kernel(const Rows<T> in, int 
 }
 
 template <typename T, bool PROBS, bool SUM>
-void launch_rows_as(const RowSource& src, int k, RowSlices cut, const RowParts& out, hipStream_t stream) {
-    hipLaunchKernelGGL((rows_kernel<T, PROBS, SUM>), dim3(cut.splits * src.rows), dim3(kThreads), 0, stream, Rows<T>(src), k, cut.splits, cut.per, out);
+void launch_rows_as(const RowSource& src, int k, int limit, RowSlices cut, const RowParts& out, hipStream_t stream) {
+    hipLaunchKernelGGL((rows_kernel<T, PROBS, SUM>), dim3(cut.splits * src.rows), dim3(kThreads), 0, stream, Rows<T>(src), k, limit, cut.splits, cut.per, out);
 }
 template <typename T, bool PROBS>
 void launch_masses_as(const RowSource& src, int pieces, int stride, double* mass, float* refs, hipStream_t stream) {
@@ -354,21 +400,29 @@ void launch_masses_as(const RowSource& src, int pieces, int stride, double* mass
 
 }  // namespace
 
-// About eight workgroups to a compute unit, slices of whole tiles, and the keys of a row's slices fit its candidates together.
-RowSlices choose_row_slices(int rows, int V, int dtype, int k) {
+// Slices of a tile at least, whose keys fit the row's candidates together.  How many: the chip holds four workgroups to a compute unit with the exponentials and five without, and
+// works them off in rounds; a slice takes its tiles and about one more for its threshold, its list and its sums.
+RowSlices choose_row_slices(int rows, int V, int dtype, int k, bool sums) {
     const long long tile = static_cast<long long>(kThreads) * kLoads * chunk_elements(dtype);
     const int tiles = static_cast<int>((static_cast<long long>(V) + chunk_elements(dtype) - 1 + tile - 1) / tile);       // wherever the row begins
-    int s = std::max(1, 2048 / rows);
-    s = std::min(std::min(s, kMaxSplits), std::min(kSelCap / k, tiles));
-    const int each = (tiles + s - 1) / s;
-    return RowSlices{(tiles + each - 1) / each, each * kThreads * kLoads};
+    const int groups = tiles * kLoads, most = std::min(std::min(kMaxSplits, kSelCap / k), tiles);     // groups: of 256 chunks
+    const long long held = 256 * (sums ? 4 : 5);
+    int best = 1;
+    long long least = -1;
+    for (int s = 1; s <= most; ++s) {
+        const int each = (groups + s - 1) / s;
+        const long long rounds = (static_cast<long long>(rows) * ((groups + each - 1) / each) + held - 1) / held, cost = rounds * (each + kLoads);
+        if (least < 0 || cost < least) { least = cost; best = s; }
+    }
+    const int each = (groups + best - 1) / best;
+    return RowSlices{(groups + each - 1) / each, each * kThreads};
 }
 
-void launch_rows(const RowSource& src, bool probs, bool sums, int k, RowSlices cut, const RowParts& out, hipStream_t stream) {
-    if (probs) launch_rows_as<float, true, true>(src, k, cut, out, stream);
-    else if (src.dtype == GR_F32) sums ? launch_rows_as<float, false, true>(src, k, cut, out, stream) : launch_rows_as<float, false, false>(src, k, cut, out, stream);
-    else if (src.dtype == GR_BF16) sums ? launch_rows_as<Bf16, false, true>(src, k, cut, out, stream) : launch_rows_as<Bf16, false, false>(src, k, cut, out, stream);
-    else sums ? launch_rows_as<_Float16, false, true>(src, k, cut, out, stream) : launch_rows_as<_Float16, false, false>(src, k, cut, out, stream);
+void launch_rows(const RowSource& src, bool probs, bool sums, int k, int limit, RowSlices cut, const RowParts& out, hipStream_t stream) {
+    if (probs) launch_rows_as<float, true, true>(src, k, limit, cut, out, stream);
+    else if (src.dtype == GR_F32) sums ? launch_rows_as<float, false, true>(src, k, limit, cut, out, stream) : launch_rows_as<float, false, false>(src, k, limit, cut, out, stream);
+    else if (src.dtype == GR_BF16) sums ? launch_rows_as<Bf16, false, true>(src, k, limit, cut, out, stream) : launch_rows_as<Bf16, false, false>(src, k, limit, cut, out, stream);
+    else sums ? launch_rows_as<_Float16, false, true>(src, k, limit, cut, out, stream) : launch_rows_as<_Float16, false, false>(src, k, limit, cut, out, stream);
 }
 
 void launch_masses(const RowSource& src, bool probs, int pieces, int stride, double* mass, float* refs, hipStream_t stream) {
