@@ -108,6 +108,18 @@ constexpr float kNone = -__builtin_inff();
 // From here on the chunk's entries are unpacked again: one instruction each, where keeping them would cost a register each.
 __device__ __forceinline__ void unpack_again(uint4& r) { asm volatile("" : "+v"(r.x), "+v"(r.y), "+v"(r.z), "+v"(r.w)); }
 
+// The largest and the smallest of a wave's values, the same in all lanes (as in gr_internal.h: no LDS round trips, all lanes active).  NaN is passed over.
+__device__ __forceinline__ float wave_max_f(float v) {
+    v = fmaxf(v, __int_as_float(dpp_move<kDppXor1>(__float_as_int(v))));
+    v = fmaxf(v, __int_as_float(dpp_move<kDppXor2>(__float_as_int(v))));
+    v = fmaxf(v, __int_as_float(dpp_move<kDppHalfMirror>(__float_as_int(v))));
+    v = fmaxf(v, __int_as_float(dpp_move<kDppMirror>(__float_as_int(v))));
+    const int b = __float_as_int(v);
+    return fmaxf(fmaxf(__int_as_float(__builtin_amdgcn_readlane(b, 0)), __int_as_float(__builtin_amdgcn_readlane(b, 16))),
+                 fmaxf(__int_as_float(__builtin_amdgcn_readlane(b, 32)), __int_as_float(__builtin_amdgcn_readlane(b, 48))));
+}
+__device__ __forceinline__ float wave_min_f(float v) { return -wave_max_f(-v); }
+
 // A row as 16-byte chunks at 16-byte boundaries, wherever it begins: chunk c holds elements [c N - lead, c N - lead + N).  Chunks that reach
 // over an end of the row are read element by element, entries outside it are -inf.
 template <typename T>
@@ -191,8 +203,7 @@ struct ExpSum {
     // from here on entries up to `most` (this lane's) come
     __device__ __forceinline__ void raise(float most, const double* tab) {
         if (__any(most > ceiling)) {
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) most = fmaxf(most, __shfl_xor(most, o));
+            most = wave_max_f(most);
             sum = rebased(most, tab);
             refer(most);
         }
@@ -228,17 +239,6 @@ struct ExpSum {
         }
     }
 };
-
-__device__ __forceinline__ float wave_max_f(float v) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v = fmaxf(v, __shfl_xor(v, o));
-    return v;
-}
-__device__ __forceinline__ float wave_min_f(float v) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v = fminf(v, __shfl_xor(v, o));
-    return v;
-}
 
 // The keys in LDS (CAP at most) cut to the k largest, in place; all threads call it.  Returns the key that they reach.
 template <int CAP, int NT = kThreads>

@@ -14,7 +14,7 @@ namespace gr {
 namespace {
 
 constexpr int kRowCap = 1024;                             // candidate keys in LDS
-constexpr int kListCap = 512;                             // chunks with candidates in LDS
+constexpr int kListCap = 1024, kWaveList = kListCap / kWaves;         // chunks with candidates in LDS, a quarter to a wave
 
 // Of the keys of a stretch of the row one that exactly k of them reach (0: no key).  Only slices with more entries at their threshold than LDS holds come
 // here (rows of equal entries, rows that rise), so the stretch is read again for every digit, and a digit that a whole wave agrees on is counted once.
@@ -63,8 +63,8 @@ __device__ __forceinline__ unsigned long long stretch_kth_largest(KeyAt key_at, 
 }
 
 // A threshold that at least k of the entries reach (-inf: there are too few), from the largest entries `top` of the threads' chunks (kLoads each, different entries): about the k-th
-// largest of them.  With 8192 entries to a tile 9 reach it for k = 8, 136 for k = 128, 290 for k = 256.  First a bound from below, the threads in G
-// groups, the smallest power of two >= k: the smallest of the groups' largest.  Then 256 linear bins from there to the largest entry.  All threads call it.
+// largest of them.  With 8192 entries to a tile 9 reach it for k = 8, 136 for k = 128, 290 for k = 256.  First a bound from below: of 64 (128, 256) groups of threads, k at
+// least, the smallest of the groups' largest.  Then 256 linear bins from there to the largest entry.  All threads call it.
 __device__ __forceinline__ float find_threshold(const float* top, int k, int* hist, float* group_max, float* edge) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     float most = top[0];
@@ -74,16 +74,10 @@ __device__ __forceinline__ float find_threshold(const float* top, int k, int* hi
     __syncthreads();                                      // whoever reads what an earlier call left is done
     hist[tid] = 0;
     if (lane == 0) edge[kWaves + wave] = hi;
-    if (k <= 64) {
-        int groups = 1;
-        while (groups < k) groups *= 2;
-        for (int o = 32; o >= groups; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
-        group_max[tid] = most;
-        __syncthreads();
-        lo = wave_min_f(fmaxf(fmaxf(group_max[lane], group_max[lane + 64]), fmaxf(group_max[lane + 128], group_max[lane + 192])));
-    } else {
-        group_max[tid] = most;
-        __syncthreads();
+    group_max[tid] = most;
+    __syncthreads();
+    if (k <= 64) lo = wave_min_f(fmaxf(fmaxf(group_max[lane], group_max[lane + 64]), fmaxf(group_max[lane + 128], group_max[lane + 192])));
+    else {
         lo = wave_min_f(k <= 128 ? fmaxf(most, group_max[tid ^ 128]) : most);
         if (lane == 0) edge[wave] = lo;
         __syncthreads();
@@ -127,7 +121,7 @@ __global__ __launch_bounds__(kThreads, SUM && !PROBS ? 4 : 5) void rows_kernel(c
     __shared__ int list_chunk[kListCap];
     __shared__ int hist[256];
     __shared__ int pick[4];
-    __shared__ int count, listed;
+    __shared__ int count, listed[kWaves];
     __shared__ float group_max[kThreads];
     __shared__ double red[kWaves];
     __shared__ float edge[2 * kWaves];
@@ -160,7 +154,8 @@ __global__ __launch_bounds__(kThreads, SUM && !PROBS ? 4 : 5) void rows_kernel(c
         if (!(temp > 0.f) || !(temp <= 3.0e38f)) bad = 1; else scale = kPerTemp / static_cast<double>(temp);
         fill_exp_table(tab);
     }
-    if (tid == 0) { count = 0; listed = 0; }
+    if (tid == 0) count = 0;
+    int mine_listed = 0;                                  // chunks on the wave's own quarter of the list
     __syncthreads();
 
     float theta = kNone;                                  // entries below it are no candidates
@@ -171,14 +166,21 @@ __global__ __launch_bounds__(kThreads, SUM && !PROBS ? 4 : 5) void rows_kernel(c
     const auto key_of = [](float v, int id) { return PROBS ? make_key(v, id) : make_key_logit(v, id); };
     // the list taken apart: its entries that reach the threshold become keys
     const auto work_off = [&]() {
+        if (lane == 0) listed[wave] = mine_listed;
+        mine_listed = 0;
         __syncthreads();
-        const int n = listed;
-        over = over || n > kListCap;
+        int n[kWaves], upto_wave[kWaves], all = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) { n[w] = listed[w]; over = over || n[w] > kWaveList; all += min(n[w], kWaveList); upto_wave[w] = all; }
 #pragma unroll
         for (int r = 0; r < kListCap / kThreads; ++r) {
-            const int i = tid + r * kThreads;
-            const bool have = i < min(n, kListCap);
+            // the i-th chunk of the four quarters one after the other
+            const int i0 = tid + r * kThreads;
+            const bool have = i0 < all;
             if (!__any(have)) break;
+            int i = i0;
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) if (i0 >= upto_wave[w - 1]) i = w * kWaveList + i0 - upto_wave[w - 1];
             const uint4 raw = have ? list[i] : make_uint4(0u, 0u, 0u, 0u);
             const int chunk = have ? list_chunk[i] : 0;
             unsigned mask = 0u;
@@ -199,9 +201,10 @@ __global__ __launch_bounds__(kThreads, SUM && !PROBS ? 4 : 5) void rows_kernel(c
         over = over || count > kRowCap;
     };
 
-    // The first tile's threshold lies at about its k-th entry, give or take 1 / sqrt(k) of its rank: six times that much has room for so many tiles.  Later ones hold
-    // ever fewer candidates, so the stretches double.
-    int refresh = max(1, kListCap / (k + 6 * static_cast<int>(sqrtf(static_cast<float>(k))) + 12)), tiles = 0;
+    // The first tile's threshold lies at about its k-th entry, give or take 1 / sqrt(k) of its rank, and a wave finds a quarter of them, give or take its root: six times that
+    // much has room for so many tiles.  Later ones hold ever fewer candidates, so the stretches double.
+    const float wave_k = 0.25f * static_cast<float>(k);
+    int refresh = max(1, static_cast<int>(kWaveList / (wave_k + 6.f * sqrtf(wave_k) + 8.f))), tiles = 0;
     for (int c0 = c_first; c0 < c_end; c0 += kTileChunks) {
         uint4 now[kLoads];
 #pragma unroll
@@ -252,15 +255,14 @@ __global__ __launch_bounds__(kThreads, SUM && !PROBS ? 4 : 5) void rows_kernel(c
 #pragma unroll
         for (int l = 0; l < kLoads; ++l) { hit[l] = __ballot(top[l] >= theta && top[l] > least); hits += __popcll(hit[l]); }
         if (hits != 0) {
-            int slot = 0;
-            if (lane == 0) slot = atomicAdd(&listed, hits);
-            slot = __builtin_amdgcn_readfirstlane(slot);
+            int slot = mine_listed;
 #pragma unroll
             for (int l = 0; l < kLoads; ++l) {
-                const int mine = slot + __builtin_amdgcn_mbcnt_hi(static_cast<unsigned>(hit[l] >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<unsigned>(hit[l]), 0u));
-                if ((hit[l] >> lane & 1ull) && mine < kListCap) { list[mine] = now[l]; list_chunk[mine] = c0 + l * kThreads + tid; }
+                const int at = slot + __builtin_amdgcn_mbcnt_hi(static_cast<unsigned>(hit[l] >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<unsigned>(hit[l]), 0u));
+                if ((hit[l] >> lane & 1ull) && at < kWaveList) { list[wave * kWaveList + at] = now[l]; list_chunk[wave * kWaveList + at] = c0 + l * kThreads + tid; }
                 slot += __popcll(hit[l]);
             }
+            mine_listed = slot;
         }
         if (++tiles == refresh && c0 + kTileChunks < c_end) {
             refresh *= 2;
@@ -272,7 +274,6 @@ __global__ __launch_bounds__(kThreads, SUM && !PROBS ? 4 : 5) void rows_kernel(c
                 thin_keys<kRowCap, PROBS>(keys, c, k, kRowCap / 2, hist, pick, edge, &count, &reach);
                 theta = fmaxf(theta, reach);
             }
-            if (tid == 0) listed = 0;
             __syncthreads();
         }
     }
@@ -299,22 +300,29 @@ __global__ __launch_bounds__(kThreads, SUM && !PROBS ? 4 : 5) void rows_kernel(c
         found = k;
     } else if (found > room) found = thin_keys<kRowCap, PROBS>(keys, found, k, room, hist, pick, edge, &count);
     for (int i = tid; i < found; i += kThreads) to[i] = keys[i];
-    double sum = 0.0;
-    float ref = 0.f;
-    if (SUM && PROBS) sum = block_sum(total, red);
-    if (kExp) {
-        __syncthreads();
-        if (lane == 0) edge[wave] = es.ref;
-        __syncthreads();
-        ref = fmaxf(fmaxf(edge[0], edge[1]), fmaxf(edge[2], edge[3]));
-        bad |= static_cast<int>(!(es.sum == es.sum));
-        sum = block_sum(es.rebased(ref, tab), red);
-    }
-    const int any_bad = block_sum_i(bad, red);
-    if (tid == 0) {
-        const int at = row * splits + s;
-        out.count[at] = found; out.bad[at] = any_bad;
-        if (SUM) { out.sum[at] = sum; if (!PROBS) out.ref[at] = ref; }
+    // the waves' sums: of exponentials, to the largest of their references
+    __syncthreads();
+    if (kExp) bad |= static_cast<int>(!(es.sum == es.sum));
+    const double wave_total = SUM ? wave_sum(kExp ? es.sum : total) : 0.0;
+    const bool wave_bad = __any(bad != 0);
+    if (lane == 0) { red[wave] = wave_total; edge[wave] = es.ref; pick[wave] = wave_bad; }
+    __syncthreads();
+    if (tid < kWaves) {
+        // a lane to a wave's sum
+        float ref = es.ref;
+        double sum = red[tid];
+        if (kExp) {
+            es.ref = edge[tid]; es.sum = sum;
+            ref = fmaxf(fmaxf(edge[0], edge[1]), fmaxf(edge[2], edge[3]));
+            sum = es.rebased(ref, tab);
+        }
+        sum += __shfl_xor(sum, 1);
+        sum += __shfl_xor(sum, 2);
+        if (tid == 0) {
+            const int at = row * splits + s;
+            out.count[at] = found; out.bad[at] = pick[0] | pick[1] | pick[2] | pick[3];
+            if (SUM) { out.sum[at] = sum; if (!PROBS) out.ref[at] = ref; }
+        }
     }
 }
 
