@@ -8,6 +8,7 @@ namespace gr {
 namespace {
 
 constexpr int kMergeThreads = 512, kMergeWaves = kMergeThreads / 64, kMergeCap = 1024;
+static_assert(GR_MAX_BEAMS * kMaxSplits <= 2048, "beam_of");
 constexpr int kMaxLists = GR_MAX_BEAMS * kMaxSplits;
 constexpr int kHeldLists = 8;                             // lists of a wave whose keys are on their way at once
 constexpr int kBatchKeys = kMergeWaves * GR_MAX_BEAMS;    // a wave to a slice's list, at most GR_MAX_BEAMS keys each
@@ -18,9 +19,10 @@ struct MergeLds {
     unsigned long long value[kMergeCap], key[kMergeCap];  // candidates: the score as a rising pattern, (logit, ~id)
     int beam[kMergeCap];
     int lists[kMaxLists];                                 // keys in the list of (beam, slice)
-    float refs[kMaxLists]; double sums[kMaxLists];
     double top[GR_MAX_BEAMS], log_sum[GR_MAX_BEAMS], score[GR_MAX_BEAMS];
     double best[kMergeThreads];
+    double edge[kMergeWaves];
+    int hist[256];
     int count, bad;
 };
 
@@ -29,39 +31,48 @@ __device__ __forceinline__ bool ahead(unsigned long long va, int ba, unsigned lo
     return va != vb ? va > vb : (ba != bb ? ba < bb : ka > kb);
 }
 
-// The candidates in LDS cut to the best M, in order, by counting; `parts` threads side by side to a candidate where there are few.
-__device__ void keep_best(MergeLds& L, int c, int M) {
-    const int tid = threadIdx.x;
-    constexpr int kEach = kMergeCap / kMergeThreads;
-    unsigned long long v[kEach] = {}, k[kEach] = {};
-    int b[kEach] = {}, rank[kEach];
-    int parts = 1;
-    while (parts < 64 && c * parts * 2 <= kMergeThreads) parts *= 2;
-    const int part = tid % parts;
+// The candidates in LDS cut to the best M, in order.  A wave holds the scores of all in its lanes and takes an eighth of them in turn: its rank is the number of set bits of the comparison of
+// all with it; where scores are equal, which is rare, the rest is compared one by one.
+__device__ __forceinline__ void keep_best(MergeLds& L, int c, int M) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    c = __builtin_amdgcn_readfirstlane(c);                // the same in all lanes, and known to be
+    constexpr int kRegs = kMergeCap / 64;
+    with_registers<kRegs>(c, [&](auto regs) {
+        constexpr int R = decltype(regs)::value;
+        unsigned long long v[R], k[R];
+        int b[R], rank[R];
 #pragma unroll
-    for (int r = 0; r < kEach; ++r) {
-        const int i = (tid + r * kMergeThreads) / parts;
-        rank[r] = kMergeCap;
-        if (r > 0 && i >= c) break;                       // with more than one part a second round has nobody
-        if (i < c) { v[r] = L.value[i]; k[r] = L.key[i]; b[r] = L.beam[i]; }
-        int before = 0;
-        for (int j0 = part; j0 < c; j0 += 8 * parts) {
-            unsigned long long other[8];                  // eight reads on their way at once
+        for (int r = 0; r < R; ++r) {
+            const int i = r * 64 + lane;
+            const bool have = i < c;
+            v[r] = have ? L.value[i] : 0ull;              // 0: below every score
+            k[r] = have ? L.key[i] : 0ull; b[r] = have ? L.beam[i] : 0;
+        }
+        int ties = 0;
 #pragma unroll
-            for (int u = 0; u < 8; ++u) other[u] = L.value[min(j0 + u * parts, c - 1)];
+        for (int r = 0; r < R; ++r) {
+            rank[r] = kMergeCap;                          // of the lane's own candidate, where it is the wave's turn
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const int j = j0 + u * parts;
-                if (j < c && other[u] >= v[r]) before += static_cast<int>(ahead(other[u], L.beam[j], L.key[j], v[r], b[r], k[r]));
+            for (int turn = 0; turn < 64 / kMergeWaves; ++turn) {
+                const int at = turn * kMergeWaves + wave;
+                const unsigned long long mine = read_lane64(v[r], at);
+                int before = 0, same = 0;
+#pragma unroll
+                for (int o = 0; o < R; ++o) { before += __popcll(__ballot(v[o] > mine)); same += __popcll(__ballot(v[o] == mine)); }
+                rank[r] = lane == at ? before : rank[r];
+                ties |= static_cast<int>(mine != 0ull) & static_cast<int>(same > 1);
             }
         }
-        for (int o = 1; o < parts; o <<= 1) before += __shfl_xor(before, o);
-        if (i < c && part == 0) rank[r] = before;
-    }
-    __syncthreads();
+        if (ties) {
 #pragma unroll
-    for (int r = 0; r < kEach; ++r)
-        if (rank[r] < M) { L.value[rank[r]] = v[r]; L.key[rank[r]] = k[r]; L.beam[rank[r]] = b[r]; }
+            for (int r = 0; r < R; ++r)
+                if (rank[r] != kMergeCap && v[r] != 0ull)
+                    for (int j = 0; j < c; ++j) rank[r] += static_cast<int>(L.value[j] == v[r] && ahead(v[r], L.beam[j], L.key[j], v[r], b[r], k[r]));
+        }
+        __syncthreads();                                  // all have read
+#pragma unroll
+        for (int r = 0; r < R; ++r) if (rank[r] < M && v[r] != 0ull) { L.value[rank[r]] = v[r]; L.key[rank[r]] = k[r]; L.beam[rank[r]] = b[r]; }
+    });
     if (tid == 0) L.count = min(c, M);
     __syncthreads();
 }
@@ -70,37 +81,49 @@ __device__ void keep_best(MergeLds& L, int c, int M) {
 // M-th best, from groups of threads, leaves some dozens, which are put in order by counting.
 // Bound: a chain of steps behind one read.  What the slices left lies in other chips' L2, a microsecond away, so counts, sums and keys are all asked for at the
 // beginning, keys before it is known how many there are (each list after the other took 25 us for 64 lists).
-__global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(const Rows<float> in, int K, int M, int eos, int splits, const RowParts parts, const BeamOut out) {
+__global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(const Rows<float> in, int K, int M, int eos, int splits, int inverse, const RowParts parts, const BeamOut out) {
     __shared__ MergeLds L;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, seq = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), seq = blockIdx.x;
     const int row0 = seq * K, lists = K * splits, room = kSelCap / splits, most = min(room, GR_MAX_BEAMS);
+    const auto beam_of = [&](int list) { return (list * inverse) >> 16; };        // list / splits: inverse is 2^16 / splits, rounded up; exact below 2^11 lists
     // lanes take turns at being the first of a list, so that every group of lanes meets candidates
     const auto place = [&](int list) { return (lane + list * 13) & 63; };
     const auto load_key = [&](int list) -> unsigned long long {
-        const int b = list / splits, i = place(list);
+        const int b = beam_of(list), i = place(list);
         return list < lists && i < most ? parts.cand[static_cast<size_t>(row0 + b) * kSelCap + (list - b * splits) * room + i] : 0ull;
     };
     unsigned long long held[kHeldLists];                  // of lists wave, wave + 8, ..
 #pragma unroll
     for (int u = 0; u < kHeldLists; ++u) held[u] = load_key(wave + u * kMergeWaves);
     const float temp = in.temperature ? in.temperature[seq] : 1.f;
+    const double inv_temp = 1.0 / static_cast<double>(temp);
+    // a wave to a beam, a lane to a slice; of two beams everything is asked for at once
+    constexpr int kTwo = 2;
+    bool bad_beam = false;
+    for (int b0 = wave; b0 < K; b0 += kTwo * kMergeWaves) {
+        int n[kTwo], bad[kTwo]; float ref[kTwo], score[kTwo]; double sum[kTwo];
+#pragma unroll
+        for (int u = 0; u < kTwo; ++u) {
+            const int b = min(b0 + u * kMergeWaves, K - 1), at = (row0 + b) * splits + lane;
+            const bool mine = lane < splits && !in.skip(row0 + b);
+            score[u] = in.scores[row0 + b];
+            n[u] = mine ? parts.count[at] : 0; bad[u] = mine ? parts.bad[at] : 0;
+            ref[u] = mine ? parts.ref[at] : kNone; sum[u] = mine ? parts.sum[at] : 0.0;
+        }
+#pragma unroll
+        for (int u = 0; u < kTwo; ++u) {
+            const int b = b0 + u * kMergeWaves;
+            if (b >= K) break;
+            if (lane < splits) L.lists[b * splits + lane] = n[u];
+            const double top = static_cast<double>(wave_max_f(ref[u]));
+            const double total = wave_sum(ref[u] > kNone ? sum[u] * exp((static_cast<double>(ref[u]) - top) * inv_temp) : 0.0);
+            bad_beam = bad_beam || __any(bad[u] != 0) || !(score[u] < 3.0e38f);
+            if (lane == 0) { L.top[b] = top; L.log_sum[b] = log(total); L.score[b] = static_cast<double>(score[u]); }
+        }
+    }
     if (tid == 0) { L.count = 0; L.bad = 0; }
     __syncthreads();
-    for (int i = tid; i < lists; i += kMergeThreads) {
-        const int b = i / splits, at = row0 * splits + i;
-        const bool skip = in.skip(row0 + b);
-        L.lists[i] = skip ? 0 : parts.count[at];
-        L.refs[i] = skip ? kNone : parts.ref[at];
-        L.sums[i] = skip ? 0.0 : parts.sum[at];
-        if (!skip && parts.bad[at] != 0) L.bad = 1;       // any thread that sets it
-    }
-    if (tid < K) {
-        const float score = in.scores[row0 + tid];
-        L.score[tid] = static_cast<double>(score);
-        if (!(score < 3.0e38f)) L.bad = 1;
-    }
-    if (tid == 0 && (!(temp > 0.f) || !(temp <= 3.0e38f))) L.bad = 1;
-    const double inv_temp = 1.0 / static_cast<double>(temp);
+    if (lane == 0 && (bad_beam || !(temp > 0.f) || !(temp <= 3.0e38f))) L.bad = 1;       // any wave that sets it
     __syncthreads();
     const size_t at0 = static_cast<size_t>(seq) * M;
     if (L.bad) {
@@ -111,25 +134,9 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(const Rows<fl
         if (tid == 0) out.status[seq] = GR_ROW_BAD;
         return;
     }
-    // the slices' sums to the beam's largest reference: a thread to a slice
-    for (int i = tid; i < lists; i += kMergeThreads) {
-        const int b = i / splits;
-        float top = kNone;
-        for (int s = 0; s < splits; ++s) top = fmaxf(top, L.refs[b * splits + s]);
-        const float ref = L.refs[i];
-        L.sums[i] *= ref > kNone ? exp((static_cast<double>(ref) - static_cast<double>(top)) * inv_temp) : 0.0;
-        if (i == b * splits) L.top[b] = static_cast<double>(top);
-    }
-    __syncthreads();
-    if (tid < K) {
-        double sum = 0.0;
-        for (int s = 0; s < splits; ++s) sum += L.sums[tid * splits + s];
-        L.log_sum[tid] = log(sum);
-    }
-    __syncthreads();
     const auto candidate = [&](int list, unsigned long long key, double& value) -> bool {
         if (list >= lists || place(list) >= L.lists[list]) return false;
-        const int b = list / splits;
+        const int b = beam_of(list);
         value = L.score[b] + ((static_cast<double>(key_logit(key)) - L.top[b]) * inv_temp - L.log_sum[b]);
         return true;
     };
@@ -149,15 +156,32 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(const Rows<fl
     };
     double mine = kNoScore;
     each(0, lists, [&](int, unsigned long long, double value) { mine = fmax(mine, value); });
-    int groups = 1;
-    while (groups < M) groups *= 2;
-    for (int o = 32; o >= groups; o >>= 1) mine = fmax(mine, __shfl_xor(mine, o));
+    // A bound of the M-th best from below, as in find_threshold (gr_rows.hip): of 64 groups of threads the smallest of the groups' best, then 256 linear bins from
+    // there to the best of all for the threads' best: about M candidates reach the bin that holds the M-th of them.
+    const double top = wave_max(mine);
     L.best[tid] = mine;
+    if (lane == 0) L.edge[wave] = top;
+    if (tid < 256) L.hist[tid] = 0;
     __syncthreads();
-    mine = L.best[lane];
+    double group = L.best[lane], hi = L.edge[0];
 #pragma unroll
-    for (int w = 1; w < kMergeWaves; ++w) mine = fmax(mine, L.best[lane + 64 * w]);
-    double theta = wave_min(mine);
+    for (int w = 1; w < kMergeWaves; ++w) { group = fmax(group, L.best[lane + 64 * w]); hi = fmax(hi, L.edge[w]); }
+    double theta = wave_min(group);                       // -inf where some group has met none
+    const float per = 255.f / static_cast<float>(hi - theta);                    // 0, infinite or NaN where theta is -inf or all are equal: then the bins say nothing
+    const auto bin = [&](double value) { return static_cast<int>(fminf(fmaxf(static_cast<float>(value - theta) * per, 0.f), 255.f)); };       // rises with the score; NaN: 0
+    if (mine > kNoScore && mine >= theta) atomicAdd(&L.hist[bin(mine)], 1);
+    __syncthreads();
+    int held_by[4], total = 0;                            // every wave by itself: lane l owns bins 255-4l .. 252-4l
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { held_by[j] = L.hist[255 - 4 * lane - j]; total += held_by[j]; }
+    const int incl = wave_scan_i(total);
+    int above = incl - total, from = 0;
+    const bool is_mine = above < M && M <= incl;
+    if (is_mine)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { above += held_by[j]; if (from == 0 && above >= M) from = 255 - 4 * lane - j; }
+    const unsigned long long owner = __ballot(is_mine);
+    from = owner ? __builtin_amdgcn_readlane(from, __ffsll(owner) - 1) : 0;      // fewer threads than M have met any: all that reach theta
     const auto append = [&](double value, unsigned long long key, int b) {
         const int slot = atomicAdd(&L.count, 1);
         if (slot < kMergeCap) { L.value[slot] = mono64(value); L.key[slot] = key; L.beam[slot] = b; }
@@ -167,7 +191,7 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(const Rows<fl
         if (tid < K && in.finished && in.finished[row0 + tid] != 0 && L.score[tid] > kNoScore) append(L.score[tid], make_key_logit(0.f, eos), tid);
     };
     append_finished();
-    each(0, lists, [&](int list, unsigned long long key, double value) { if (value >= theta) append(value, key, list / splits); });
+    each(0, lists, [&](int list, unsigned long long key, double value) { if (value >= theta && bin(value) >= from) append(value, key, beam_of(list)); });
     __syncthreads();
     int c = L.count;
     if (c > kMergeCap) {
@@ -189,7 +213,7 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(const Rows<fl
             const int list = first + wave;
             const unsigned long long key = load_key(list);
             double value;
-            if (candidate(list, key, value) && value >= theta) append(value, key, list / splits);
+            if (candidate(list, key, value) && value >= theta) append(value, key, beam_of(list));
         }
         __syncthreads();
         c = L.count;
@@ -315,7 +339,7 @@ __global__ __launch_bounds__(kThreads) void reorder_kernel(const ReorderParams r
 }  // namespace
 
 void launch_beam_merge(const RowSource& src, int S, int K, int M, int eos, RowSlices cut, const RowParts& in, const BeamOut& out, hipStream_t stream) {
-    hipLaunchKernelGGL(beam_merge_kernel, dim3(S), dim3(kMergeThreads), 0, stream, Rows<float>(src), K, M, eos, cut.splits, in, out);
+    hipLaunchKernelGGL(beam_merge_kernel, dim3(S), dim3(kMergeThreads), 0, stream, Rows<float>(src), K, M, eos, cut.splits, (65536 + cut.splits - 1) / cut.splits, in, out);
 }
 
 void launch_reorder(const ReorderParams& params, hipStream_t stream) {

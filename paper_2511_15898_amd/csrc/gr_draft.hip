@@ -11,22 +11,35 @@ namespace gr {
 namespace {
 
 constexpr int kDraftThreads = 512, kDraftWaves = kDraftThreads / 64;
-constexpr int kPaddedSupport = 2 * kMaxSupport;           // candidates ranked at once, with what pads them to 8 `parts`; the scan's 64 behind a support
+constexpr int kRanked = 512, kRankedRegs = kRanked / 64;  // candidates put in order at once: eight to a lane
+constexpr int kSupportRegs = kMaxSupport / 64;
 
 struct DraftLds {
     unsigned long long keys[kSelCap];
-    double mass[kPaddedSupport], sum[kPaddedSupport + 1];
-    int ids[kPaddedSupport], hist[256], pick[4], count;
+    unsigned long long best[kMaxSupport];                 // by decreasing key
+    double mass[kMaxSupport + 64], sum[kMaxSupport + 64 + 1];
+    int ids[kMaxSupport], hist[256], pick[4], count;
     float edge[2 * kDraftWaves];
 };
 
-// grid = (rows), 512 threads.  The candidates are thinned to 512 at most, ranked by counting and so put in order, best first; a token's CDF is the sum of the
-// masses of the tokens up to its id, added in that order whatever the slices' order was.  Sums of more masses in one order are never smaller, so the CDF
-// rises with the id, and where nothing is added it stays the same: no sort by id and no scan is needed.
+__device__ __forceinline__ double wave_scan_d(double v) {  // inclusive, all lanes active
+    v += dpp_shift<0x111, 0xF>(v, 0.0);
+    v += dpp_shift<0x112, 0xF>(v, 0.0);
+    v += dpp_shift<0x114, 0xF>(v, 0.0);
+    v += dpp_shift<0x118, 0xF>(v, 0.0);
+    v += dpp_shift<0x142, 0xA>(v, 0.0);
+    v += dpp_shift<0x143, 0xC>(v, 0.0);
+    return v;
+}
+
+// grid = (rows), 512 threads.  The candidates are thinned to 512 at most and put in order, best first; the k best, or what the nucleus cut leaves of them, are put in order by id, and
+// a wave that has their running sums in its lanes looks up a draw.
+// In order without moving anything: every wave holds all candidates in its lanes and takes an eighth of them in turn, whose rank is the number of set bits of the comparison of all with it
+// (reading all from LDS for each of them took 22 us for 128 candidates, eight reads at once 10).
 template <bool PROBS>
 __global__ __launch_bounds__(kDraftThreads) void draft_topk_kernel(const float* __restrict__ temperature, int k, double tail_mass, int splits, const RowParts in, const DraftOut out) {
     __shared__ DraftLds L;
-    const int tid = threadIdx.x, lane = tid & 63, row = blockIdx.x, room = kSelCap / splits;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = blockIdx.x, room = kSelCap / splits;
     // the keys are asked for before it is known how many there are: what lies behind them is the handle's, too, and is not used
     constexpr int kAhead = kSelCap / kDraftThreads;
     const unsigned long long* const cand = in.cand + static_cast<size_t>(row) * kSelCap;
@@ -57,84 +70,95 @@ __global__ __launch_bounds__(kDraftThreads) void draft_topk_kernel(const float* 
     }
     __syncthreads();
     int c = found.total;
-    if (c > 2 * k + 32 || c > kPaddedSupport) c = thin_keys<kSelCap, PROBS, kDraftThreads>(L.keys, c, k, kPaddedSupport, L.hist, L.pick, L.edge, &L.count);
-    // `parts` threads to a candidate, side by side
-    int parts = 1;
-    while (parts < 64 && c * parts * 2 <= kDraftThreads) parts *= 2;
-    const int me = tid / parts, part = tid % parts;
-    const unsigned long long mine = me < c ? L.keys[me] : 0ull;
-    // eight reads on their way at once: one after the other they cost 200 cycles each
-    const int step = 8 * parts, padded = (c + step - 1) / step * step;
-    for (int i = c + tid; i < padded; i += kDraftThreads) L.keys[i] = 0ull;
-    __syncthreads();
-    int rank = 0;
-    for (int j = part; j < padded; j += step) {
-        unsigned long long key[8];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) key[u] = L.keys[j + u * parts];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) rank += static_cast<int>(key[u] > mine);
-    }
-    for (int o = 1; o < parts; o <<= 1) rank += __shfl_xor(rank, o);
-    __syncthreads();
+    if (c > 2 * k + 32 || c > kRanked) c = thin_keys<kSelCap, PROBS, kDraftThreads>(L.keys, c, k, kRanked, L.hist, L.pick, L.edge, &L.count);
+    c = __builtin_amdgcn_readfirstlane(c);                // the same in all lanes, and known to be: branches on it cost nothing
     int kk = min(c, k);
-    if (me < c && part == 0 && rank < kk) L.keys[rank] = mine;
+    with_registers<kRankedRegs>(c, [&](auto regs) {
+        constexpr int R = decltype(regs)::value;
+        unsigned long long key[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) key[r] = r * 64 + lane < c ? L.keys[r * 64 + lane] : 0ull;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            int rank = kRanked;                           // of the lane's own candidate, where it is the wave's turn
+#pragma unroll
+            for (int turn = 0; turn < 64 / kDraftWaves; ++turn) {
+                const int at = turn * kDraftWaves + wave;
+                const unsigned long long mine = read_lane64(key[r], at);
+                int before = 0;
+#pragma unroll
+                for (int o = 0; o < R; ++o) before += __popcll(__ballot(key[o] > mine));
+                rank = lane == at ? before : rank;
+            }
+            if (rank < kk && r * 64 + lane < c) L.best[rank] = key[r];
+        }
+    });
     __syncthreads();
     if (PROBS && tail_mass > 0.0) {
         // the nucleus cut of gr_solve: up to the first token at which the running sum, added one after the other, reaches (1 - tail_mass) of the row's mass
-        if (tid < kk) L.mass[tid] = static_cast<double>(key_q(L.keys[tid]));
+        if (tid < kk) L.mass[tid] = static_cast<double>(key_q(L.best[tid]));
         if (tid < 64) L.mass[kk + tid] = 0.0;             // the scan reads up to a multiple of 64
         if (tid == 0) L.count = kk;
         __syncthreads();
-        if (tid < 64) wave_sequential_scan_padded(L.mass, L.sum, kk, 0.0);
+        if (tid < 64) wave_sequential_scan_padded<16>(L.mass, L.sum, kk, 0.0);
         __syncthreads();
         if (tid < kk && L.sum[tid + 1] >= (1.0 - tail_mass) * found.qtot) atomicMin(&L.count, tid + 1);
         __syncthreads();
-        kk = L.count;
+        kk = __builtin_amdgcn_readfirstlane(L.count);
+        __syncthreads();
     }
-    for (int i = kk + tid; i < padded; i += kDraftThreads) { L.ids[i] = 0; L.mass[i] = 0.0; }
-    if (tid < kk) {
-        const unsigned long long key = L.keys[tid];
-        L.ids[tid] = key_id(key);
-        L.mass[tid] = PROBS ? static_cast<double>(key_q(key)) : exp((static_cast<double>(key_logit(key)) - static_cast<double>(key_logit(L.keys[0]))) * inv_temp);
-    }
-    __syncthreads();
-    const int id = me < kk ? L.ids[me] : -1;
-    double upto = 0.0;
-    for (int j = part; j < padded; j += step) {
-        int ids[8]; double mass[8];
+    with_registers<kSupportRegs>(kk, [&](auto regs) {
+        constexpr int R = decltype(regs)::value;
+        int id[R];
+        double mass[R];
+        const float top = key_logit(L.best[0]);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) { ids[u] = L.ids[j + u * parts]; mass[u] = L.mass[j + u * parts]; }
-#pragma unroll
-        for (int u = 0; u < 8; ++u) upto += ids[u] <= id ? mass[u] : 0.0;
-    }
-    for (int o = 1; o < parts; o <<= 1) upto += __shfl_xor(upto, o);
-    if (me < kk && part == 0) L.sum[me] = upto;
-    __syncthreads();
-    // a wave to a draw: the total is the CDF of the largest id
-    double total = 0.0;
-    for (int i = lane; i < kk; i += 64) total = fmax(total, L.sum[i]);
-    total = wave_max(total);
-    for (int d = tid >> 6; d < out.n; d += kDraftWaves) {
-        const size_t at = static_cast<size_t>(row) * out.n + d;
-        const double t = static_cast<double>(out.uniforms[at]) * total;
-        int first = 0x7FFFFFFF, last = -1;
-        for (int i = lane; i < kk; i += 64) {
-            if (L.sum[i] > t && L.mass[i] > 0.0) first = min(first, L.ids[i]);
-            if (L.mass[i] > 0.0) last = max(last, L.ids[i]);
+        for (int r = 0; r < R; ++r) {
+            const unsigned long long key = L.best[min(r * 64 + lane, kk - 1)];
+            id[r] = r * 64 + lane < kk ? key_id(key) : 0x7FFFFFFF;
+            mass[r] = PROBS ? static_cast<double>(key_q(key)) : exp((static_cast<double>(key_logit(key)) - static_cast<double>(top)) * inv_temp);
         }
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) { first = min(first, __shfl_xor(first, o)); last = max(last, __shfl_xor(last, o)); }
-        if (lane == 0) out.drafts[at] = first == 0x7FFFFFFF ? last : first;
+        for (int r = 0; r < R; ++r) {
+            int rank = kMaxSupport;
+#pragma unroll
+            for (int turn = 0; turn < 64 / kDraftWaves; ++turn) {
+                const int at = turn * kDraftWaves + wave, mine = __builtin_amdgcn_readlane(id[r], at);
+                int before = 0;
+#pragma unroll
+                for (int o = 0; o < R; ++o) before += __popcll(__ballot(id[o] < mine));
+                rank = lane == at ? before : rank;
+            }
+            if (rank < kMaxSupport && r * 64 + lane < kk) { L.ids[rank] = id[r]; L.mass[rank] = mass[r]; }
+        }
+    });
+    __syncthreads();
+    // running sums: a lane has four tokens one after the other, or fewer
+    const int per = (kk + 63) / 64, first = lane * per;
+    double cdf[kSupportRegs], own = 0.0;
+    unsigned any = 0u;
+#pragma unroll
+    for (int r = 0; r < kSupportRegs; ++r) {
+        const double m = r < per && first + r < kk ? L.mass[first + r] : 0.0;
+        own += m;
+        cdf[r] = own;
+        any |= m > 0.0 ? 1u << r : 0u;
+    }
+    const double upto = wave_scan_d(own), before = upto - own;
+    const double total = read_lane(upto, 63);
+    const unsigned long long massive = __ballot(any != 0u);
+    for (int d = wave; d < out.n; d += kDraftWaves) {
+        const size_t at = static_cast<size_t>(row) * out.n + d;
+        const double t = static_cast<double>(out.uniforms[at]) * total;
+        int mine = -1;                                    // the lane's first token of some mass whose running sum exceeds t
+#pragma unroll
+        for (int r = kSupportRegs - 1; r >= 0; --r) if ((any >> r & 1u) && before + cdf[r] > t) mine = first + r;
+        const unsigned long long over = __ballot(mine >= 0);
+        // none: rounding at the end; the last token of some mass
+        const int owner = over ? __ffsll(static_cast<unsigned long long>(over)) - 1 : 63 - __clzll(static_cast<long long>(massive));
+        if (lane == owner) out.drafts[at] = L.ids[over ? mine : first + 31 - __clz(static_cast<int>(any))];
     }
     if (tid == 0) out.status[row] = GR_ROW_OK;
-}
-
-__device__ __forceinline__ double wave_scan_d(double v) {  // inclusive, all lanes active
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) { const double w = __shfl_up(v, o); if (lane >= o) v += w; }
-    return v;
 }
 
 // grid = (rows), a wave to a draw.

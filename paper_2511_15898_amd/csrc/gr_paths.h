@@ -1,5 +1,7 @@
 // Declarations shared by the operators beside the verification: drafts drawn from rows, beams selected and moved, pages of the cache.
 #pragma once
+#include <type_traits>
+
 #include "gr_internal.h"
 
 namespace gr {
@@ -321,6 +323,21 @@ __device__ __forceinline__ int thin_keys(unsigned long long* keys, int c, int k,
     __syncthreads();
     if (reach) *reach = bin_edge(lo, hi, from);
     return left;
+}
+
+__device__ __forceinline__ unsigned long long read_lane64(unsigned long long v, int lane) {
+    return static_cast<unsigned long long>(static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(v >> 32), lane))) << 32 |
+           static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(v), lane));
+}
+// Calls use(R) with the number of registers, MOST at most, that hold `count` values in a wave's lanes, known at compile time: a branch per register and turn cost 20 cycles each.
+template <int MOST, typename Use>
+__device__ __forceinline__ void with_registers(int count, Use&& use) {
+    if (count <= 64) use(std::integral_constant<int, 1>{});
+    else if (count <= 128) use(std::integral_constant<int, 2>{});
+    else if (count <= 192) use(std::integral_constant<int, 3>{});
+    else if (MOST <= 4 || count <= 256) use(std::integral_constant<int, 4>{});
+    else if (MOST <= 6 || count <= 384) use(std::integral_constant<int, MOST < 6 ? 4 : 6>{});
+    else use(std::integral_constant<int, MOST < 6 ? 4 : MOST>{});
 }
 
 }  // namespace gr
