@@ -101,15 +101,17 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(const Rows<fl
     constexpr int kTwo = 2;
     bool bad_beam = false;
     for (int b0 = wave; b0 < K; b0 += kTwo * kMergeWaves) {
-        int n[kTwo], bad[kTwo]; float ref[kTwo], score[kTwo]; double sum[kTwo];
+        int n[kTwo], bad[kTwo]; float ref[kTwo], score[kTwo]; double sum[kTwo]; bool skip[kTwo];
 #pragma unroll
         for (int u = 0; u < kTwo; ++u) {
-            const int b = min(b0 + u * kMergeWaves, K - 1), at = (row0 + b) * splits + lane;
-            const bool mine = lane < splits && !in.skip(row0 + b);
+            // of a beam that was not read, too: what lies there is the handle's and is not used
+            const int b = min(b0 + u * kMergeWaves, K - 1), at = (row0 + b) * splits + min(lane, splits - 1);
+            skip[u] = in.skip(row0 + b);
             score[u] = in.scores[row0 + b];
-            n[u] = mine ? parts.count[at] : 0; bad[u] = mine ? parts.bad[at] : 0;
-            ref[u] = mine ? parts.ref[at] : kNone; sum[u] = mine ? parts.sum[at] : 0.0;
+            n[u] = parts.count[at]; bad[u] = parts.bad[at]; ref[u] = parts.ref[at]; sum[u] = parts.sum[at];
         }
+#pragma unroll
+        for (int u = 0; u < kTwo; ++u) if (lane >= splits || skip[u]) { n[u] = 0; bad[u] = 0; ref[u] = kNone; sum[u] = 0.0; }
 #pragma unroll
         for (int u = 0; u < kTwo; ++u) {
             const int b = b0 + u * kMergeWaves;
@@ -140,22 +142,23 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(const Rows<fl
         value = L.score[b] + ((static_cast<double>(key_logit(key)) - L.top[b]) * inv_temp - L.log_sum[b]);
         return true;
     };
-    // calls use(list, key, value) for every candidate of lists from `first` on, `count` of them
-    const auto each = [&](int first, int count, auto&& use) {
-        for (int l0 = first; l0 < first + count; l0 += kHeldLists * kMergeWaves) {
-            if (first != 0 || l0 != 0 || lists > kHeldLists * kMergeWaves)
+    // Calls use(list, key, value) for every candidate.  Up to 64 lists stay in registers, keys and scores.
+    double scores_held[kHeldLists];
+    const bool all_held = lists <= kHeldLists * kMergeWaves;
+    const auto each = [&](bool again, auto&& use) {
+        for (int l0 = 0; l0 < lists; l0 += kHeldLists * kMergeWaves) {
+            if (!all_held)
 #pragma unroll
                 for (int u = 0; u < kHeldLists; ++u) held[u] = load_key(l0 + wave + u * kMergeWaves);
+            if (!all_held || !again)
 #pragma unroll
-            for (int u = 0; u < kHeldLists; ++u) {
-                const int list = l0 + wave + u * kMergeWaves;
-                double value;
-                if (list < first + count && candidate(list, held[u], value)) use(list, held[u], value);
-            }
+                for (int u = 0; u < kHeldLists; ++u) if (!candidate(l0 + wave + u * kMergeWaves, held[u], scores_held[u])) scores_held[u] = kNoScore;
+#pragma unroll
+            for (int u = 0; u < kHeldLists; ++u) if (scores_held[u] > kNoScore) use(l0 + wave + u * kMergeWaves, held[u], scores_held[u]);
         }
     };
     double mine = kNoScore;
-    each(0, lists, [&](int, unsigned long long, double value) { mine = fmax(mine, value); });
+    each(false, [&](int, unsigned long long, double value) { mine = fmax(mine, value); });
     // A bound of the M-th best from below, as in find_threshold (gr_rows.hip): of 64 groups of threads the smallest of the groups' best, then 256 linear bins from
     // there to the best of all for the threads' best: about M candidates reach the bin that holds the M-th of them.
     const double top = wave_max(mine);
@@ -191,7 +194,7 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(const Rows<fl
         if (tid < K && in.finished && in.finished[row0 + tid] != 0 && L.score[tid] > kNoScore) append(L.score[tid], make_key_logit(0.f, eos), tid);
     };
     append_finished();
-    each(0, lists, [&](int list, unsigned long long key, double value) { if (value >= theta && bin(value) >= from) append(value, key, beam_of(list)); });
+    each(true, [&](int list, unsigned long long key, double value) { if (value >= theta && bin(value) >= from) append(value, key, beam_of(list)); });
     __syncthreads();
     int c = L.count;
     if (c > kMergeCap) {
