@@ -507,7 +507,9 @@ int draft_rows(gr_handle h, const RowSource& src, bool probs, int n, int k, cons
     if ((!all && k_eff > kMaxSupport) || (h->tail_mass > 0.0 && (!probs || k_eff > kMaxSupport))) return GR_EUNSUPPORTED;
     h->solved = false;                                   // the selection scratch of the handle is overwritten
     const DraftOut out{uniforms, n, drafts, status};
-    if (k_eff <= kMaxSupport) {
+    if (k_eff <= kMaxSupport && draft_in_one(src.rows, src.V, src.dtype)) {
+        launch_draft_rows(src, probs, k_eff, h->tail_mass, out, stream);
+    } else if (k_eff <= kMaxSupport) {
         const RowSlices cut = choose_row_slices(src.rows, src.V, src.dtype, k_eff, false);
         const RowParts parts{h->cand, h->cand_count, h->part_psum, h->part_pref, h->part_bad};
         launch_rows(src, probs, false, k_eff, kSelCap, cut, parts, stream);
@@ -515,9 +517,12 @@ int draft_rows(gr_handle h, const RowSource& src, bool probs, int n, int k, cons
         launch_draft_topk(src, probs, k_eff, h->tail_mass, cut, parts, out, stream);
     } else {
         const int pieces = piece_count(src.V, src.dtype);
-        launch_masses(src, probs, pieces, h->piece_stride, h->piece_psum, h->piece_pref, stream);
-        if (hipGetLastError() != hipSuccess) return GR_EHIP;
-        launch_draft_whole(src, probs, pieces, h->piece_stride, h->piece_psum, h->piece_pref, out, stream);
+        if (draft_whole_in_one(src.rows, src.V, src.dtype, probs)) launch_draft_whole_rows(src, probs, pieces, out, stream);
+        else {
+            launch_masses(src, probs, pieces, h->piece_stride, h->piece_psum, h->piece_pref, stream);
+            if (hipGetLastError() != hipSuccess) return GR_EHIP;
+            launch_draft_whole(src, probs, pieces, h->piece_stride, h->piece_psum, h->piece_pref, out, stream);
+        }
     }
     return hipGetLastError() != hipSuccess ? GR_EHIP : GR_OK;
 }

@@ -45,6 +45,12 @@ void launch_masses(const RowSource& src, bool probs, int pieces, int stride, dou
 
 // Drafts.  Of rows cut to their k largest: from what launch_rows left; of whole rows: from what launch_masses left.
 struct DraftOut { const float* uniforms; int n; int* drafts; int* status; };
+constexpr int kComputeUnits = 256;                        // of an MI355X
+constexpr int kLdsPieces = 2048;                          // piece sums of a row that one workgroup reads
+bool draft_in_one(int rows, int V, int dtype);
+void launch_draft_rows(const RowSource& src, bool probs, int k, double tail_mass, const DraftOut& out, hipStream_t stream);
+bool draft_whole_in_one(int rows, int V, int dtype, bool probs);
+void launch_draft_whole_rows(const RowSource& src, bool probs, int pieces, const DraftOut& out, hipStream_t stream);
 void launch_draft_topk(const RowSource& src, bool probs, int k, double tail_mass, RowSlices cut, const RowParts& in, const DraftOut& out, hipStream_t stream);
 void launch_draft_whole(const RowSource& src, bool probs, int pieces, int stride, const double* mass, const float* refs, const DraftOut& out, hipStream_t stream);
 

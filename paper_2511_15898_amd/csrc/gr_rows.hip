@@ -7,27 +7,29 @@
 // rows the exponentials and the read take about the same time, so both have to overlap.
 #include <algorithm>
 
-#include "gr_paths.h"
+#include "gr_draft.h"
 
 namespace gr {
 
 namespace {
 
-constexpr int kRowCap = 1024;                             // candidate keys in LDS
-constexpr int kListCap = 1024, kWaveList = kListCap / kWaves;         // chunks with candidates in LDS, a quarter to a wave
+// What a scan of NT threads keeps in LDS: candidate keys, chunks with candidates (a share to every wave).
+template <int NT> constexpr int kRowCap = NT <= 256 ? 1024 : 2048;
+template <int NT> constexpr int kListCap = NT <= 256 ? 1024 : 2048;
+template <int NT> constexpr int kWaveList = kListCap<NT> / (NT / 64);
 
-// Of the keys of a stretch of the row one that exactly k of them reach (0: no key).  Only slices with more entries at their threshold than LDS holds come
+// Of the keys of a stretch of the row one that exactly k of them reach (0, as ruled out entries: fewer than k).  Only slices with more entries at their threshold than LDS holds come
 // here (rows of equal entries, rows that rise), so the stretch is read again for every digit, and a digit that a whole wave agrees on is counted once.
-template <typename KeyAt>
+template <int NT, typename KeyAt>
 __device__ __forceinline__ unsigned long long stretch_kth_largest(KeyAt key_at, int count, int k, int* hist, int* pick) {
     const int tid = threadIdx.x;
     unsigned long long prefix = 0;
     int need = k;
     for (int shift = 56; shift >= 0; shift -= 8) {
-        hist[tid] = 0;
+        if (tid < 256) hist[tid] = 0;
         __syncthreads();
         const unsigned long long mask = (shift == 56) ? 0ull : (~0ull << (shift + 8));
-        for (int i = tid; i < count; i += kThreads) {
+        for (int i = tid; i < count; i += NT) {
             const unsigned long long key = key_at(i);
             if (key != 0ull && (key & mask) == prefix) {
                 const int digit = static_cast<int>((key >> shift) & 255ull);
@@ -51,6 +53,7 @@ __device__ __forceinline__ unsigned long long stretch_kth_largest(KeyAt key_at, 
                     above += c[j];
                 }
             }
+            if (tid == 63 && incl < need) { pick[0] = 0; pick[1] = 0; pick[2] = 0; }         // fewer than k: at the first digit only
         }
         __syncthreads();
         prefix |= static_cast<unsigned long long>(pick[0]) << shift;
@@ -65,25 +68,38 @@ __device__ __forceinline__ unsigned long long stretch_kth_largest(KeyAt key_at, 
 // A threshold that at least k of the entries reach (-inf: there are too few), from the largest entries `top` of the threads' chunks (kLoads each, different entries): about the k-th
 // largest of them.  With 8192 entries to a tile 9 reach it for k = 8, 136 for k = 128, 290 for k = 256.  First a bound from below: of 64 (128, 256) groups of threads, k at
 // least, the smallest of the groups' largest.  Then 256 linear bins from there to the largest entry.  All threads call it.
+template <int NT>
 __device__ __forceinline__ float find_threshold(const float* top, int k, int* hist, float* group_max, float* edge) {
+    constexpr int kNW = NT / 64;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     float most = top[0];
 #pragma unroll
     for (int l = 1; l < kLoads; ++l) most = fmaxf(most, top[l]);
-    float lo, hi = wave_max_f(most);
+    float hi = wave_max_f(most);
     __syncthreads();                                      // whoever reads what an earlier call left is done
-    hist[tid] = 0;
-    if (lane == 0) edge[kWaves + wave] = hi;
+    if (tid < 256) hist[tid] = 0;
+    if (lane == 0) edge[wave] = hi;
     group_max[tid] = most;
     __syncthreads();
-    if (k <= 64) lo = wave_min_f(fmaxf(fmaxf(group_max[lane], group_max[lane + 64]), fmaxf(group_max[lane + 128], group_max[lane + 192])));
-    else {
-        lo = wave_min_f(k <= 128 ? fmaxf(most, group_max[tid ^ 128]) : most);
-        if (lane == 0) edge[wave] = lo;
-        __syncthreads();
-        lo = fminf(fminf(edge[0], edge[1]), fminf(edge[2], edge[3]));
-    }
-    hi = fmaxf(fmaxf(edge[4], edge[5]), fmaxf(edge[6], edge[7]));
+    // group g: the threads whose number is g modulo 64 (128, 256); a lane looks after groups lane, lane + 64, ..
+    float lo;
+    const auto bound = [&](auto groups) {
+        constexpr int G = decltype(groups)::value;
+        float least = __builtin_inff();
+#pragma unroll
+        for (int q = 0; q < G; q += 64) {
+            float m = kNone;
+#pragma unroll
+            for (int j = 0; j < NT; j += G) m = fmaxf(m, group_max[lane + q + j]);
+            least = fminf(least, m);
+        }
+        lo = wave_min_f(least);
+    };
+    if (k <= 64) bound(std::integral_constant<int, 64>{});
+    else if (k <= 128) bound(std::integral_constant<int, 128>{});
+    else bound(std::integral_constant<int, 256>{});
+#pragma unroll
+    for (int w = 0; w < kNW; ++w) hi = fmaxf(hi, edge[w]);
     if (!(lo > kNone)) return kNone;                      // the same for all threads
     const float per = 255.f / (hi - lo);
 #pragma unroll
@@ -112,37 +128,37 @@ __device__ __forceinline__ float find_threshold(const float* top, int k, int* hi
 // exponential, with the listed chunks in float64, was measured: %F32%, but sums good to 2e-8 only, which depend on how a row is cut.)
 // Rows of beams that are not in use or finished are not read (Rows::skip).
 // Four waves to a SIMD with the exponentials: for a fifth their loop spills (32 us become 37, 89 become 114).
-template <typename T, bool PROBS, bool SUM>
-__global__ __launch_bounds__(kThreads, SUM && !PROBS ? 4 : 5) void rows_kernel(const Rows<T> in, int k, int limit, int splits, int per, const RowParts out) {
-    constexpr int N = Packed<T>::N, kTileChunks = kThreads * kLoads;
-    constexpr bool kExp = SUM && !PROBS;
-    __shared__ unsigned long long keys[kRowCap];
-    __shared__ uint4 list[kListCap];
-    __shared__ int list_chunk[kListCap];
-    __shared__ int hist[256];
-    __shared__ int pick[4];
-    __shared__ int count, listed[kWaves];
-    __shared__ float group_max[kThreads];
-    __shared__ double red[kWaves];
-    __shared__ float edge[2 * kWaves];
-    __shared__ double tab[kExp ? kExpEntries : 1];
+template <bool EXP, int NT>
+struct ScanLds {
+    unsigned long long keys[kRowCap<NT>];
+    uint4 list[kListCap<NT>];
+    int list_chunk[kListCap<NT>];
+    int hist[256], pick[4], count, listed[NT / 64];
+    float group_max[NT], edge[2 * (NT / 64)];
+    double red[NT / 64], tab[EXP ? kExpEntries : 1];
+};
+// What a thread has of a slice behind a scan: how many keys lie in LDS (the same for all), whether it met a bad entry, its part of the sum (with its wave's reference).
+struct Scanned { int found, bad; double total; ExpSum es; };
 
+template <typename T, bool PROBS, bool EXP, int NT>
+__device__ __forceinline__ Scanned scan_slice(ScanLds<EXP, NT>& L, const Rows<T>& in, int row, const RowChunks<T>& x, int c_first, int c_end, int k) {
+    constexpr int N = Packed<T>::N, kTileChunks = NT * kLoads, kNW = NT / 64, kCap = kRowCap<NT>;
+    constexpr bool kExp = EXP;
+    unsigned long long* const keys = L.keys;
+    uint4* const list = L.list; int* const list_chunk = L.list_chunk; int* const hist = L.hist; int* const pick = L.pick; int* const listed = L.listed;
+    int& count = L.count;
+    float* const edge = L.edge; double* const tab = L.tab;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int row = blockIdx.x / splits, s = blockIdx.x - row * splits;
-    if (in.skip(row)) return;
-    const RowChunks<T> x(in.row(row), in.V);
-    const int c_first = s * per, c_end = min(x.chunks, c_first + per);
-
     uint4 next[kLoads];
     const auto fetch = [&](int c0) {
         if (c0 + kTileChunks <= c_end && x.inside(c0, c0 + kTileChunks)) {
 #pragma unroll
-            for (int l = 0; l < kLoads; ++l) next[l] = x.load(c0, l * kThreads + tid);
+            for (int l = 0; l < kLoads; ++l) next[l] = x.load(c0, l * NT + tid);
         } else if (c0 < c_end)
 #pragma unroll
             for (int l = 0; l < kLoads; ++l) {
-                const int c = c0 + l * kThreads;
-                if (c + kThreads <= c_end && x.inside(c, c + kThreads)) next[l] = x.load(c, tid);
+                const int c = c0 + l * NT;
+                if (c + NT <= c_end && x.inside(c, c + NT)) next[l] = x.load(c, tid);
                 else if (c < c_end) next[l] = x.load_guarded(c + tid < c_end ? c + tid : x.chunks);
             }
     };
@@ -152,10 +168,10 @@ __global__ __launch_bounds__(kThreads, SUM && !PROBS ? 4 : 5) void rows_kernel(c
     if (kExp) {
         const float temp = in.temperature_of(row);
         if (!(temp > 0.f) || !(temp <= 3.0e38f)) bad = 1; else scale = kPerTemp / static_cast<double>(temp);
-        fill_exp_table(tab);
+        if (tid < kExpEntries) fill_exp_table(tab);
     }
     if (tid == 0) count = 0;
-    int mine_listed = 0;                                  // chunks on the wave's own quarter of the list
+    int mine_listed = 0;                                  // chunks on the wave's own share of the list
     __syncthreads();
 
     float theta = kNone;                                  // entries below it are no candidates
@@ -169,18 +185,18 @@ __global__ __launch_bounds__(kThreads, SUM && !PROBS ? 4 : 5) void rows_kernel(c
         if (lane == 0) listed[wave] = mine_listed;
         mine_listed = 0;
         __syncthreads();
-        int n[kWaves], upto_wave[kWaves], all = 0;
+        int n[kNW], upto_wave[kNW], all = 0;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) { n[w] = listed[w]; over = over || n[w] > kWaveList; all += min(n[w], kWaveList); upto_wave[w] = all; }
+        for (int w = 0; w < kNW; ++w) { n[w] = listed[w]; over = over || n[w] > kWaveList<NT>; all += min(n[w], kWaveList<NT>); upto_wave[w] = all; }
 #pragma unroll
-        for (int r = 0; r < kListCap / kThreads; ++r) {
-            // the i-th chunk of the four quarters one after the other
-            const int i0 = tid + r * kThreads;
+        for (int r = 0; r < kListCap<NT> / NT; ++r) {
+            // the i-th chunk of the waves' shares one after the other
+            const int i0 = tid + r * NT;
             const bool have = i0 < all;
             if (!__any(have)) break;
             int i = i0;
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) if (i0 >= upto_wave[w - 1]) i = w * kWaveList + i0 - upto_wave[w - 1];
+            for (int w = 1; w < kNW; ++w) if (i0 >= upto_wave[w - 1]) i = w * kWaveList<NT> + i0 - upto_wave[w - 1];
             const uint4 raw = have ? list[i] : make_uint4(0u, 0u, 0u, 0u);
             const int chunk = have ? list_chunk[i] : 0;
             unsigned mask = 0u;
@@ -195,22 +211,22 @@ __global__ __launch_bounds__(kThreads, SUM && !PROBS ? 4 : 5) void rows_kernel(c
             int slot = __builtin_amdgcn_readlane(base, 63) + upto - __popc(mask);
 #pragma unroll
             for (int j = 0; j < N; ++j)
-                if (mask >> j & 1u) { if (slot < kRowCap) keys[slot] = key_of(Packed<T>::get(raw, j), x.id(chunk, j)); ++slot; }
+                if (mask >> j & 1u) { if (slot < kCap) keys[slot] = key_of(Packed<T>::get(raw, j), x.id(chunk, j)); ++slot; }
         }
         __syncthreads();
-        over = over || count > kRowCap;
+        over = over || count > kCap;
     };
 
-    // The first tile's threshold lies at about its k-th entry, give or take 1 / sqrt(k) of its rank, and a wave finds a quarter of them, give or take its root: six times that
+    // The first tile's threshold lies at about its k-th entry, give or take 1 / sqrt(k) of its rank, and a wave finds its share of them, give or take the root: six times that
     // much has room for so many tiles.  Later ones hold ever fewer candidates, so the stretches double.
-    const float wave_k = 0.25f * static_cast<float>(k);
-    int refresh = max(1, static_cast<int>(kWaveList / (wave_k + 6.f * sqrtf(wave_k) + 8.f))), tiles = 0;
+    const float wave_k = static_cast<float>(k) / kNW;
+    int refresh = max(1, static_cast<int>(kWaveList<NT> / (wave_k + 6.f * sqrtf(wave_k) + 8.f))), tiles = 0;
     for (int c0 = c_first; c0 < c_end; c0 += kTileChunks) {
         uint4 now[kLoads];
 #pragma unroll
         for (int l = 0; l < kLoads; ++l) now[l] = next[l];
         fetch(c0 + kTileChunks);
-        const int loads = min(kLoads, (c_end - c0 + kThreads - 1) / kThreads);     // of the last tile maybe fewer
+        const int loads = min(kLoads, (c_end - c0 + NT - 1) / NT);     // of the last tile maybe fewer
         // Entries outside the row are -inf.  Bad: NaN, +inf (logits), negative entries (probabilities).
         float top[kLoads], most = kNone, probe = 0.f;
 #pragma unroll
@@ -249,7 +265,7 @@ __global__ __launch_bounds__(kThreads, SUM && !PROBS ? 4 : 5) void rows_kernel(c
                     es.add(v, tab);
                 }
         }
-        if (theta == kNone) theta = find_threshold(top, k, hist, group_max, edge);
+        if (theta == kNone) theta = find_threshold<NT>(top, k, hist, L.group_max, edge);
         unsigned long long hit[kLoads];
         int hits = 0;
 #pragma unroll
@@ -259,7 +275,7 @@ __global__ __launch_bounds__(kThreads, SUM && !PROBS ? 4 : 5) void rows_kernel(c
 #pragma unroll
             for (int l = 0; l < kLoads; ++l) {
                 const int at = slot + __builtin_amdgcn_mbcnt_hi(static_cast<unsigned>(hit[l] >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<unsigned>(hit[l]), 0u));
-                if ((hit[l] >> lane & 1ull) && at < kWaveList) { list[wave * kWaveList + at] = now[l]; list_chunk[wave * kWaveList + at] = c0 + l * kThreads + tid; }
+                if ((hit[l] >> lane & 1ull) && at < kWaveList<NT>) { list[wave * kWaveList<NT> + at] = now[l]; list_chunk[wave * kWaveList<NT> + at] = c0 + l * NT + tid; }
                 slot += __popcll(hit[l]);
             }
             mine_listed = slot;
@@ -271,15 +287,13 @@ __global__ __launch_bounds__(kThreads, SUM && !PROBS ? 4 : 5) void rows_kernel(c
             __syncthreads();
             if (!over && c > k) {
                 float reach;
-                thin_keys<kRowCap, PROBS>(keys, c, k, kRowCap / 2, hist, pick, edge, &count, &reach);
+                thin_keys<kCap, PROBS, NT>(keys, c, k, kCap / 2, hist, pick, edge, &count, &reach);
                 theta = fmaxf(theta, reach);
             }
             __syncthreads();
         }
     }
     work_off();
-    const int room = min(kSelCap / splits, limit);        // k at least
-    unsigned long long* const to = out.cand + static_cast<size_t>(row) * kSelCap + s * (kSelCap / splits);
     int found = count;
     __syncthreads();
     if (over) {
@@ -289,61 +303,99 @@ __global__ __launch_bounds__(kThreads, SUM && !PROBS ? 4 : 5) void rows_kernel(c
             const float e = Packed<T>::one(x.row[e0 + i]);
             return e > least ? key_of(e, static_cast<int>(e0 + i)) : 0ull;
         };
-        const unsigned long long reach = stretch_kth_largest(slice_key, static_cast<int>(e1 - e0), k, hist, pick);
+        const unsigned long long reach = stretch_kth_largest<NT>(slice_key, static_cast<int>(e1 - e0), k, hist, pick);
         if (tid == 0) count = 0;
         __syncthreads();
-        for (int i = tid; i < static_cast<int>(e1 - e0); i += kThreads) {
+        for (int i = tid; i < static_cast<int>(e1 - e0); i += NT) {
             const unsigned long long key = slice_key(i);
             if (key >= reach && key != 0ull) keys[atomicAdd(&count, 1)] = key;
         }
         __syncthreads();
-        found = k;
-    } else if (found > room) found = thin_keys<kRowCap, PROBS>(keys, found, k, room, hist, pick, edge, &count);
-    for (int i = tid; i < found; i += kThreads) to[i] = keys[i];
+        found = count;                                    // k, or all that there are
+        __syncthreads();
+    }
+    return Scanned{found, bad, total, es};
+}
+
+template <typename T, bool PROBS, bool SUM>
+__global__ __launch_bounds__(kThreads, SUM && !PROBS ? 4 : 5) void rows_kernel(const Rows<T> in, int k, int limit, int splits, int per, const RowParts out) {
+    constexpr bool kExp = SUM && !PROBS;
+    __shared__ ScanLds<kExp, kThreads> L;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int row = blockIdx.x / splits, s = blockIdx.x - row * splits;
+    if (in.skip(row)) return;
+    const RowChunks<T> x(in.row(row), in.V);
+    Scanned mine = scan_slice<T, PROBS, kExp, kThreads>(L, in, row, x, s * per, min(x.chunks, s * per + per), k);
+    int found = mine.found;
+    const int room = min(kSelCap / splits, limit);        // k at least
+    unsigned long long* const to = out.cand + static_cast<size_t>(row) * kSelCap + s * (kSelCap / splits);
+    if (found > room) found = thin_keys<kRowCap<kThreads>, PROBS>(L.keys, found, k, room, L.hist, L.pick, L.edge, &L.count);
+    for (int i = tid; i < found; i += kThreads) to[i] = L.keys[i];
     // the waves' sums: of exponentials, to the largest of their references
     __syncthreads();
-    if (kExp) bad |= static_cast<int>(!(es.sum == es.sum));
-    const double wave_total = SUM ? wave_sum(kExp ? es.sum : total) : 0.0;
-    const bool wave_bad = __any(bad != 0);
-    if (lane == 0) { red[wave] = wave_total; edge[wave] = es.ref; pick[wave] = wave_bad; }
+    if (kExp) mine.bad |= static_cast<int>(!(mine.es.sum == mine.es.sum));
+    const double wave_total = SUM ? wave_sum(kExp ? mine.es.sum : mine.total) : 0.0;
+    const bool wave_bad = __any(mine.bad != 0);
+    if (lane == 0) { L.red[wave] = wave_total; L.edge[wave] = mine.es.ref; L.pick[wave] = wave_bad; }
     __syncthreads();
     if (tid < kWaves) {
         // a lane to a wave's sum
-        float ref = es.ref;
-        double sum = red[tid];
+        float ref = mine.es.ref;
+        double sum = L.red[tid];
         if (kExp) {
-            es.ref = edge[tid]; es.sum = sum;
-            ref = fmaxf(fmaxf(edge[0], edge[1]), fmaxf(edge[2], edge[3]));
-            sum = es.rebased(ref, tab);
+            mine.es.ref = L.edge[tid]; mine.es.sum = sum;
+            ref = fmaxf(fmaxf(L.edge[0], L.edge[1]), fmaxf(L.edge[2], L.edge[3]));
+            sum = mine.es.rebased(ref, L.tab);
         }
         sum += __shfl_xor(sum, 1);
         sum += __shfl_xor(sum, 2);
         if (tid == 0) {
             const int at = row * splits + s;
-            out.count[at] = found; out.bad[at] = pick[0] | pick[1] | pick[2] | pick[3];
+            out.count[at] = found; out.bad[at] = L.pick[0] | L.pick[1] | L.pick[2] | L.pick[3];
             if (SUM) { out.sum[at] = sum; if (!PROBS) out.ref[at] = ref; }
         }
     }
 }
 
-// The sums of a row by pieces: a wave to 64 * kLoads chunks one after the other.  grid = (pieces / 4 * rows).  PROBS: sums of the entries; logits: sums of
-// exp((x - ref) / T) with the piece's largest entry as ref.
-template <typename T, bool PROBS>
-__global__ __launch_bounds__(kThreads) void masses_kernel(const Rows<T> in, int pieces, int stride, double* __restrict__ mass, float* __restrict__ refs) {
-    constexpr int N = Packed<T>::N;
-    __shared__ double tab[PROBS ? 1 : kExpEntries];
-    const int tid = threadIdx.x, lane = tid & 63, groups = (pieces + kWaves - 1) / kWaves, row = blockIdx.x / groups;
+// The drafts of rows that one workgroup each reads: grid = (rows), NT threads.  No slices to join, so one launch does, and the candidates never leave LDS.
+template <typename T, bool PROBS, int NT>
+__global__ __launch_bounds__(NT) void draft_rows_kernel(const Rows<T> in, int k, double tail_mass, const DraftOut out) {
+    __shared__ union { ScanLds<false, NT> scan; DraftLds<kRowCap<NT>, NT> draft; } L;       // the keys are the first of both
+    static_assert(offsetof(decltype(L.scan), keys) == 0 && offsetof(decltype(L.draft), keys) == 0 && sizeof(L.scan.keys) == sizeof(L.draft.keys));
+    __shared__ double q_wave[NT / 64];
+    __shared__ int bad_wave[NT / 64];
+    const int tid = threadIdx.x, lane = tid & 63, row = blockIdx.x;
     const RowChunks<T> x(in.row(row), in.V);
-    int bad = 0;
-    double scale = 0.0;
-    if (!PROBS) {
-        const float temp = in.temperature_of(row);
-        if (!(temp > 0.f) || !(temp <= 3.0e38f)) bad = 1; else scale = kPerTemp / static_cast<double>(temp);
-        fill_exp_table(tab);
-        __syncthreads();
+    const Scanned mine = scan_slice<T, PROBS, false, NT>(L.scan, in, row, x, 0, x.chunks, k);
+    const double q_mine = PROBS ? wave_sum(mine.total) : 0.0;
+    const bool bad_mine = __any(mine.bad != 0);
+    if (lane == 0) { q_wave[tid >> 6] = q_mine; bad_wave[tid >> 6] = bad_mine; }
+    __syncthreads();
+    double q_total = 0.0, inv_temp = 1.0;
+    bool bad = mine.found == 0;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) { q_total += q_wave[w]; bad = bad || bad_wave[w] != 0; }
+    if (PROBS) bad = bad || !(fabs(q_total - 1.0) <= 1e-3);
+    else {
+        const float t = in.temperature_of(row);
+        if (!(t > 0.f) || !(t <= 3.0e38f)) bad = true; else inv_temp = 1.0 / static_cast<double>(t);
     }
-    const int piece = (blockIdx.x - row * groups) * kWaves + (tid >> 6);
-    if (piece >= pieces) return;                          // whole waves
+    if (bad) {                                            // the same for all threads
+        if (tid < out.n) out.drafts[static_cast<size_t>(row) * out.n + tid] = -1;
+        if (tid == 0) out.status[row] = GR_ROW_BAD;
+        return;
+    }
+    draw_from<PROBS>(L.draft, mine.found, k, tail_mass, q_total, inv_temp, row, out);
+}
+
+// The sum of piece `piece` of a row, a wave's 64 * kLoads chunks one after the other; all lanes hold it.  PROBS: of the entries; logits: of exp((x - ref) / T) with the piece's
+// largest entry as ref, scale 0 for a bad temperature.  A bad entry makes it NaN, and with it the row's total.
+struct PieceMass { double mass; float ref; };
+template <typename T, bool PROBS>
+__device__ __forceinline__ PieceMass piece_mass(const RowChunks<T>& x, int piece, double scale, const double* tab) {
+    constexpr int N = Packed<T>::N;
+    const int lane = threadIdx.x & 63;
+    int bad = static_cast<int>(!(scale > 0.0));
     const int c0 = piece * 64 * kLoads;
     uint4 r[kLoads];
     if (x.inside(c0, c0 + 64 * kLoads))
@@ -390,16 +442,68 @@ __global__ __launch_bounds__(kThreads) void masses_kernel(const Rows<T> in, int 
         }
     }
     sum = wave_sum(sum);
-    const unsigned long long any_bad = __ballot(bad != 0);
-    if (lane == 0) {
+    return PieceMass{__any(bad != 0) ? __builtin_nan("") : sum, ref};
+}
+template <typename T>
+__device__ __forceinline__ double scale_of(const Rows<T>& in, int row) {
+    const float temp = in.temperature_of(row);
+    return (temp > 0.f) && (temp <= 3.0e38f) ? kPerTemp / static_cast<double>(temp) : 0.0;
+}
+
+// The sums of a row by pieces, a wave to a piece.  grid = (pieces / 4 * rows).
+template <typename T, bool PROBS>
+__global__ __launch_bounds__(kThreads) void masses_kernel(const Rows<T> in, int pieces, int stride, double* __restrict__ mass, float* __restrict__ refs) {
+    __shared__ double tab[PROBS ? 1 : kExpEntries];
+    const int tid = threadIdx.x, groups = (pieces + kWaves - 1) / kWaves, row = blockIdx.x / groups;
+    if (!PROBS) { fill_exp_table(tab); __syncthreads(); }
+    const int piece = (blockIdx.x - row * groups) * kWaves + (tid >> 6);
+    if (piece >= pieces) return;                          // whole waves
+    const PieceMass m = piece_mass<T, PROBS>(RowChunks<T>(in.row(row), in.V), piece, PROBS ? 1.0 : scale_of(in, row), tab);
+    if ((tid & 63) == 0) {
         const size_t at = static_cast<size_t>(row) * stride + piece;
-        mass[at] = any_bad ? __builtin_nan("") : sum; refs[at] = ref;          // a bad entry makes the row's total NaN
+        mass[at] = m.mass; refs[at] = m.ref;
     }
+}
+
+// Sums and draws of rows that one workgroup each reads, in one launch; the sums by pieces stay in LDS.  grid = (rows), NT threads.
+template <typename T, bool PROBS, int NT>
+__global__ __launch_bounds__(NT) void draft_whole_rows_kernel(const Rows<T> in, int pieces, const DraftOut out) {
+    __shared__ double tab[PROBS ? 1 : kExpEntries], mass[kLdsPieces];
+    __shared__ float refs[kLdsPieces];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = blockIdx.x;
+    if (!PROBS) { if (tid < kExpEntries) fill_exp_table(tab); __syncthreads(); }
+    const RowChunks<T> x(in.row(row), in.V);
+    const double scale = PROBS ? 1.0 : scale_of(in, row);
+    for (int piece = wave; piece < pieces; piece += NT / 64) {
+        const PieceMass m = piece_mass<T, PROBS>(x, piece, scale, tab);
+        if ((tid & 63) == 0) { mass[piece] = m.mass; refs[piece] = m.ref; }
+    }
+    __syncthreads();
+    for (int draw = wave; draw < out.n; draw += NT / 64) draw_whole<T, PROBS>(in, row, draw, pieces, mass, refs, out);
 }
 
 template <typename T, bool PROBS, bool SUM>
 void launch_rows_as(const RowSource& src, int k, int limit, RowSlices cut, const RowParts& out, hipStream_t stream) {
     hipLaunchKernelGGL((rows_kernel<T, PROBS, SUM>), dim3(cut.splits * src.rows), dim3(kThreads), 0, stream, Rows<T>(src), k, limit, cut.splits, cut.per, out);
+}
+template <typename T, bool PROBS>
+void launch_draft_rows_as(const RowSource& src, int k, double tail_mass, const DraftOut& out, hipStream_t stream) {
+    const auto run = [&](auto threads) {
+        constexpr int NT = decltype(threads)::value;
+        hipLaunchKernelGGL((draft_rows_kernel<T, PROBS, NT>), dim3(src.rows), dim3(NT), 0, stream, Rows<T>(src), k, tail_mass, out);
+    };
+    if (src.rows <= kComputeUnits) run(std::integral_constant<int, 1024>{});
+    else if (src.rows <= 2 * kComputeUnits) run(std::integral_constant<int, 512>{});
+    else run(std::integral_constant<int, 256>{});
+}
+template <typename T, bool PROBS>
+void launch_draft_whole_rows_as(const RowSource& src, int pieces, const DraftOut& out, hipStream_t stream) {
+    const auto run = [&](auto threads) {
+        constexpr int NT = decltype(threads)::value;
+        hipLaunchKernelGGL((draft_whole_rows_kernel<T, PROBS, NT>), dim3(src.rows), dim3(NT), 0, stream, Rows<T>(src), pieces, out);
+    };
+    if (src.rows <= kComputeUnits) run(std::integral_constant<int, 1024>{});
+    else run(std::integral_constant<int, 512>{});
 }
 template <typename T, bool PROBS>
 void launch_masses_as(const RowSource& src, int pieces, int stride, double* mass, float* refs, hipStream_t stream) {
@@ -414,7 +518,7 @@ RowSlices choose_row_slices(int rows, int V, int dtype, int k, bool sums) {
     const long long tile = static_cast<long long>(kThreads) * kLoads * chunk_elements(dtype);
     const int tiles = static_cast<int>((static_cast<long long>(V) + chunk_elements(dtype) - 1 + tile - 1) / tile);       // wherever the row begins
     const int groups = tiles * kLoads, most = std::min(std::min(kMaxSplits, kSelCap / k), tiles);     // groups: of 256 chunks
-    const long long held = 256 * (sums ? 4 : 5);
+    const long long held = kComputeUnits * (sums ? 4 : 5);
     int best = 1;
     long long least = -1;
     for (int s = 1; s <= most; ++s) {
@@ -426,11 +530,42 @@ RowSlices choose_row_slices(int rows, int V, int dtype, int k, bool sums) {
     return RowSlices{(groups + each - 1) / each, each * kThreads};
 }
 
+// Whether a workgroup to a row takes less time than slices that a second launch joins: where the row is short (three tiles of 1024 threads), and where there are rows enough to occupy
+// half the chip.  Measured, split against whole, us per call: one row of 32000 in float32 14.4, 11.2; 256 of them 17.5, 13.2; one of 128256 in bfloat16 14.1, 15.3, 64 of them 15.0, 15.9,
+// 128 of them 18.5, 16.5, 256 of them 24.0, 21.5; of 151936 in float32 one 15.3, 21.3, 128 24.6, 25.6, 256 35.7, 34.0.
+// As many threads as let all rows be read at the same time, 1024 to a compute unit, or, past 512 rows, 256, of which five workgroups fit: 1024 rows of 32000 in bfloat16 take 29.5
+// in slices, 43.1 with 1024 threads, 27.0 with 512, 21.8 with 256; 320 rows 17.3, 20.4, 13.5, 14.8.
+bool draft_in_one(int rows, int V, int dtype) {
+    return rows >= kComputeUnits / 2 || static_cast<long long>(V) <= 3ll * 1024 * kLoads * chunk_elements(dtype);
+}
+
+// The same for draws from whole rows.  Short: 32768 logits (their exponentials take longer than the read) or 65536 probabilities.  Measured, two launches against one: a row of 16384 logits
+// in float32 10.7, 8.3, of 32768 10.7, 10.5, of 50021 11.2, 12.9, of 65536 in bfloat16 13.1, 15.7; of 65536 probabilities 9.9, 8.3, of 98304 10.0, 10.7.  192 rows and more: 203 of
+// 50021 probabilities, 16 draws each, 14.5, 10.7; 203 of 128256 in bfloat16 34.7, 36.3, 256 of them 38.6, 37.2; 256 of 151936 in float32 43.7, 37.3.  More rows than compute units: with
+// 512 threads 1024 rows of 16384 in float32 take 22.4, with 1024 threads 25.6, in two launches 26.3; 4096 of 2048 44.4, 56.3, 41.0.
+bool draft_whole_in_one(int rows, int V, int dtype, bool probs) {
+    return piece_count(V, dtype) <= kLdsPieces && (4 * rows >= 3 * kComputeUnits || V <= (probs ? 65536 : 32768));
+}
+
 void launch_rows(const RowSource& src, bool probs, bool sums, int k, int limit, RowSlices cut, const RowParts& out, hipStream_t stream) {
     if (probs) launch_rows_as<float, true, true>(src, k, limit, cut, out, stream);
     else if (src.dtype == GR_F32) sums ? launch_rows_as<float, false, true>(src, k, limit, cut, out, stream) : launch_rows_as<float, false, false>(src, k, limit, cut, out, stream);
     else if (src.dtype == GR_BF16) sums ? launch_rows_as<Bf16, false, true>(src, k, limit, cut, out, stream) : launch_rows_as<Bf16, false, false>(src, k, limit, cut, out, stream);
     else sums ? launch_rows_as<_Float16, false, true>(src, k, limit, cut, out, stream) : launch_rows_as<_Float16, false, false>(src, k, limit, cut, out, stream);
+}
+
+void launch_draft_rows(const RowSource& src, bool probs, int k, double tail_mass, const DraftOut& out, hipStream_t stream) {
+    if (probs) launch_draft_rows_as<float, true>(src, k, tail_mass, out, stream);
+    else if (src.dtype == GR_F32) launch_draft_rows_as<float, false>(src, k, 0.0, out, stream);
+    else if (src.dtype == GR_BF16) launch_draft_rows_as<Bf16, false>(src, k, 0.0, out, stream);
+    else launch_draft_rows_as<_Float16, false>(src, k, 0.0, out, stream);
+}
+
+void launch_draft_whole_rows(const RowSource& src, bool probs, int pieces, const DraftOut& out, hipStream_t stream) {
+    if (probs) launch_draft_whole_rows_as<float, true>(src, pieces, out, stream);
+    else if (src.dtype == GR_F32) launch_draft_whole_rows_as<float, false>(src, pieces, out, stream);
+    else if (src.dtype == GR_BF16) launch_draft_whole_rows_as<Bf16, false>(src, pieces, out, stream);
+    else launch_draft_whole_rows_as<_Float16, false>(src, pieces, out, stream);
 }
 
 void launch_masses(const RowSource& src, bool probs, int pieces, int stride, double* mass, float* refs, hipStream_t stream) {

@@ -259,3 +259,69 @@ def test_drafts_leave_no_policy_and_refuse_what_they_cannot_do(torch, gr):
                 call()
     finally:
         gr.gr_destroy(h); gr.gr_destroy(cut)
+
+
+# Rows at which the bookkeeping of a pass over a row is at its limits: few or many, short or long, so that they are read by one workgroup of either size or in slices.
+SHAPES = [(2, 9001), (1, 49152), (2, 70001), (260, 6000), (515, 5003)]
+
+
+@pytest.mark.parametrize("B,V", SHAPES + [(1, 300007), (130, 100003)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("k", [3, 256])
+@pytest.mark.parametrize("kind", ["rising", "steps", "equal"])
+def test_rows_that_keep_more_candidates_than_there_is_room_for(torch, gr, B, V, dtype, k, kind):
+    """Rows that rise (every later entry beats the threshold of the first), that rise in steps, and rows of equal entries."""
+    i = torch.arange(V, device="cuda", dtype=torch.float32)
+    row = {"rising": i * (8.0 / V), "steps": torch.floor(i / 700) % 64, "equal": torch.zeros(V, device="cuda")}[kind]
+    x = row.to(getattr(torch, dtype))[None].repeat(B, 1)
+    x[B - 1] = x[B - 1].flip(0)                                      # and one that falls
+    u = _uniforms(V, B, 4)
+    h = gr.gr_create(B, V, max_n=4)
+    try:
+        drafts, status = gr.gr_draft_logits(h, x, torch.ones(B, device="cuda"), 4, k, torch.from_numpy(u).cuda())
+        assert int(status.abs().sum()) == ROW_OK
+        drafts, x = drafts.cpu().numpy(), x.float().cpu().numpy()
+        some = sorted({0, B // 2, B - 1})
+        _check(drafts[some], x[some], k, u[some], lambda row, ids, b: softmax_mass(row[ids], 1.0))
+    finally:
+        gr.gr_destroy(h)
+
+
+@pytest.mark.parametrize("B", [1, 300, 600])
+@pytest.mark.parametrize("few", [1, 130, 200, 255, 256, 257])
+@pytest.mark.parametrize("first", [0, 1283, 5 * 256])
+def test_few_unmasked_tokens_close_together(torch, gr, B, few, first):
+    """All but `few` entries are masked, and those lie one to a 16-byte chunk in one stretch: fewer than k of 256, or as many, in the hands of few threads."""
+    V, k = 20000, 256
+    x = torch.full((B, V), -float("inf"), device="cuda")
+    at = first + 4 * torch.arange(few, device="cuda")
+    x[:, at] = torch.randn((B, few), device="cuda", generator=torch.Generator(device="cuda").manual_seed(few))
+    u = _uniforms(few, B, 3)
+    h = gr.gr_create(B, V, max_n=3)
+    try:
+        drafts, status = gr.gr_draft_logits(h, x, torch.ones(B, device="cuda"), 3, k, torch.from_numpy(u).cuda())
+        assert int(status.abs().sum()) == ROW_OK
+        some = sorted({0, B // 2, B - 1})
+        _check(drafts[some].cpu().numpy(), x[some].cpu().numpy(), k, u[some], lambda row, ids, b: softmax_mass(row[ids], 1.0))
+    finally:
+        gr.gr_destroy(h)
+
+
+@pytest.mark.parametrize("probs", [True, False])
+@pytest.mark.parametrize("B,V,n", [(1, 32768, 16), (2, 65537, 5), (1, 300007, 16), (192, 20011, 3), (256, 5000, 16), (257, 5000, 16), (700, 1025, 2)])
+def test_whole_rows_few_and_many_short_and_long(torch, gr, probs, B, V, n):
+    x = _logits(V + B, B, V, "mild")
+    if probs:
+        e = np.exp(x.astype(np.float64))
+        x = (e / e.sum(1, keepdims=True)).astype(np.float32)
+    u = _uniforms(B, B, n)
+    h = gr.gr_create(B, V, max_n=n)
+    try:
+        cx, cu = torch.from_numpy(x).cuda(), torch.from_numpy(u).cuda()
+        drafts, status = gr.gr_draft(h, cx, n, 0, cu) if probs else gr.gr_draft_logits(h, cx, torch.ones(B, device="cuda"), n, 0, cu)
+        assert int(status.abs().sum()) == ROW_OK
+        some = sorted({0, B // 3, B - 1})
+        _check(drafts[some].cpu().numpy(), x[some], 0, u[some],
+               (lambda row, ids, b: row[ids].astype(np.float64)) if probs else (lambda row, ids, b: softmax_mass(row[ids], 1.0)))
+    finally:
+        gr.gr_destroy(h)
