@@ -28,13 +28,25 @@ struct DraftLds {
     float edge[2 * (NT / 64)];
 };
 
+// The uniforms of a wave's draws: asked for before the row is read, a microsecond that nobody waits for then.
+template <int NT>
+struct Uniforms {
+    static constexpr int kNW = NT / 64, kMost = (GR_MAX_N + kNW - 1) / kNW;
+    float of[kMost];
+    __device__ __forceinline__ Uniforms(const DraftOut& out, int row) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) of[i] = out.uniforms[static_cast<size_t>(row) * out.n + min(wave + i * kNW, out.n - 1)];
+    }
+};
+
 // n independent draws from c candidates, c > 0, of which the k largest count, by inverse CDF over ascending token ids, one uniform per draw.  The candidates are thinned to 512
 // at most and put in order, best first; the k best, or what the nucleus cut leaves of them, are put in order by id, and a wave that has their running sums in its lanes looks up a draw.
 // In order without moving anything: every wave holds all candidates in its lanes and takes its share of them in turn, whose rank is the number of set bits of the comparison of all with it
 // (reading all from LDS for each of them took 22 us for 128 candidates, eight reads at once 10; so 8).
 // Masses and their sums are float64: a draw is a whole number, and next to a border of the CDF float32 sums would move some.
 template <bool PROBS, int CAP, int NT>
-__device__ __forceinline__ void draw_from(DraftLds<CAP, NT>& L, int c, int k, double tail_mass, double q_total, double inv_temp, int row, const DraftOut& out) {
+__device__ __forceinline__ void draw_from(DraftLds<CAP, NT>& L, int c, int k, double tail_mass, double q_total, double inv_temp, const Uniforms<NT>& uniforms, int row, const DraftOut& out) {
     constexpr int kNW = NT / 64;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     if (c > 2 * k + 32 || c > kRanked) c = thin_keys<CAP, PROBS, NT>(L.keys, c, k, kRanked, L.hist, L.pick, L.edge, &L.count);
@@ -114,9 +126,12 @@ __device__ __forceinline__ void draw_from(DraftLds<CAP, NT>& L, int c, int k, do
     const double upto = wave_scan_d(own), before = upto - own;
     const double total = read_lane(upto, 63);
     const unsigned long long massive = __ballot(any != 0u);
-    for (int d = wave; d < out.n; d += kNW) {
+#pragma unroll
+    for (int i = 0; i < Uniforms<NT>::kMost; ++i) {
+        const int d = wave + i * kNW;
+        if (d >= out.n) break;
         const size_t at = static_cast<size_t>(row) * out.n + d;
-        const double t = static_cast<double>(out.uniforms[at]) * total;
+        const double t = static_cast<double>(uniforms.of[i]) * total;
         int mine = -1;                                    // the lane's first token of some mass whose running sum exceeds t
 #pragma unroll
         for (int r = kSupportRegs - 1; r >= 0; --r) if ((any >> r & 1u) && before + cdf[r] > t) mine = first + r;

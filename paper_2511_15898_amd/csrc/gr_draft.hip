@@ -26,14 +26,14 @@ __global__ __launch_bounds__(kDraftThreads) void draft_topk_kernel(const float* 
         const int i = r * kDraftThreads + tid;
         ahead[r] = i < splits * room ? cand[i] : 0ull;
     }
+    const Uniforms<kDraftThreads> uniforms(out, row);
+    const float t = PROBS ? 1.f : temperature[row];
     const SliceTotals found = slice_totals<false>(in.count, in.bad, in.sum, in.sum, nullptr, row, splits, 0.0);
     bool bad = found.bad != 0 || found.total == 0;
     double inv_temp = 1.0;
     if (PROBS) bad = bad || !(fabs(found.qtot - 1.0) <= 1e-3);
-    else {
-        const float t = temperature[row];
-        if (!(t > 0.f) || !(t <= 3.0e38f)) bad = true; else inv_temp = 1.0 / static_cast<double>(t);
-    }
+    else if (!(t > 0.f) || !(t <= 3.0e38f)) bad = true;
+    else inv_temp = 1.0 / static_cast<double>(t);
     if (bad) {                                            // the same for all threads
         if (tid < out.n) out.drafts[static_cast<size_t>(row) * out.n + tid] = -1;
         if (tid == 0) out.status[row] = GR_ROW_BAD;
@@ -46,7 +46,7 @@ __global__ __launch_bounds__(kDraftThreads) void draft_topk_kernel(const float* 
         if (at < count) L.keys[before + at] = ahead[r];   // at < room: i lies in slice s (behind the last one none counts)
     }
     __syncthreads();
-    draw_from<PROBS>(L, found.total, k, tail_mass, found.qtot, inv_temp, row, out);
+    draw_from<PROBS>(L, found.total, k, tail_mass, found.qtot, inv_temp, uniforms, row, out);
 }
 
 // grid = (rows), a wave to a draw.

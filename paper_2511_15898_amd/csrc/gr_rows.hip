@@ -366,6 +366,8 @@ __global__ __launch_bounds__(NT) void draft_rows_kernel(const Rows<T> in, int k,
     __shared__ int bad_wave[NT / 64];
     const int tid = threadIdx.x, lane = tid & 63, row = blockIdx.x;
     const RowChunks<T> x(in.row(row), in.V);
+    const Uniforms<NT> uniforms(out, row);
+    const float t = PROBS ? 1.f : in.temperature_of(row);
     const Scanned mine = scan_slice<T, PROBS, false, NT>(L.scan, in, row, x, 0, x.chunks, k);
     const double q_mine = PROBS ? wave_sum(mine.total) : 0.0;
     const bool bad_mine = __any(mine.bad != 0);
@@ -376,16 +378,14 @@ __global__ __launch_bounds__(NT) void draft_rows_kernel(const Rows<T> in, int k,
 #pragma unroll
     for (int w = 0; w < NT / 64; ++w) { q_total += q_wave[w]; bad = bad || bad_wave[w] != 0; }
     if (PROBS) bad = bad || !(fabs(q_total - 1.0) <= 1e-3);
-    else {
-        const float t = in.temperature_of(row);
-        if (!(t > 0.f) || !(t <= 3.0e38f)) bad = true; else inv_temp = 1.0 / static_cast<double>(t);
-    }
+    else if (!(t > 0.f) || !(t <= 3.0e38f)) bad = true;
+    else inv_temp = 1.0 / static_cast<double>(t);
     if (bad) {                                            // the same for all threads
         if (tid < out.n) out.drafts[static_cast<size_t>(row) * out.n + tid] = -1;
         if (tid == 0) out.status[row] = GR_ROW_BAD;
         return;
     }
-    draw_from<PROBS>(L.draft, mine.found, k, tail_mass, q_total, inv_temp, row, out);
+    draw_from<PROBS>(L.draft, mine.found, k, tail_mass, q_total, inv_temp, uniforms, row, out);
 }
 
 // The sum of piece `piece` of a row, a wave's 64 * kLoads chunks one after the other; all lanes hold it.  PROBS: of the entries; logits: of exp((x - ref) / T) with the piece's
