@@ -166,14 +166,23 @@ struct RowChunks {
 // the table's upper words have j 2^12 taken off.  Ten instructions behind the float64 argument and one read of the table.  (A table of 32 entries without bank conflicts
 // and degree 3: 15.)  In two steps, so that several reads are on their way before the first is used.
 constexpr int kExpEntries = 256;
+constexpr double kExpMagic = 6755399441055744.0;         // 1.5 * 2^52
 struct ExpPart { double rest, entry; int whole; };
 __device__ __forceinline__ ExpPart exp2_256_begin(double y, const double* tab) {
-    constexpr double kMagic = 6755399441055744.0;
-    const double m = y + kMagic;
+    const double m = y + kExpMagic;
     ExpPart e;
     e.whole = __double2loint(m);
     e.entry = tab[e.whole & (kExpEntries - 1)];
-    e.rest = y - (m - kMagic);
+    e.rest = y - (m - kExpMagic);
+    return e;
+}
+// The same for y = x scale + shift with a whole shift, from shift + 1.5 * 2^52, which is exact: one operation less, and the rest is rounded once.
+__device__ __forceinline__ ExpPart exp2_256_begin(double x, double scale, double shift_magic, const double* tab) {
+    const double m = fma(x, scale, shift_magic);
+    ExpPart e;
+    e.whole = __double2loint(m);
+    e.entry = tab[e.whole & (kExpEntries - 1)];
+    e.rest = fma(x, scale, shift_magic - m);
     return e;
 }
 __device__ __forceinline__ double exp2_256_end(const ExpPart& e, double sum) {
@@ -188,24 +197,29 @@ __device__ __forceinline__ void fill_exp_table(double* tab) {        // by 256 t
     tab[threadIdx.x] = __hiloint2double(__double2hiint(v) - (threadIdx.x << 12), __double2loint(v));
 }
 
-// A wave's sum of exponentials: of exp((x - ref) / T), ref the largest entry of its first tile that has any.  A later entry may lie above ref (float64
-// has room for e^433 of them) until that is used up; then the sum is brought to a new reference.
+// A wave's sum of exponentials: of exp((x - ref) / T), but for a factor near 1, ref the largest entry of its first tile that has any.  A later entry may lie above ref
+// (float64 has room for e^433 of them) until that is used up; then the sum is brought to a new reference.
 struct ExpSum {
-    double sum = 0.0, scale, shift = 0.0;                 // scale: kPerTemp / T; shift: -ref * scale
+    double sum = 0.0, scale, shift = 0.0;                 // of 2^(place(x) / 256); scale: kPerTemp / T; shift: -ref * scale, rounded to a whole number
     float ref = kNone, floor = kNone, ceiling = kNone;    // floor: entries below it count as if they were e^-474 of the reference; above the ceiling there is no room
-    bool plain = false;                                   // ref * scale is small enough for its rounding
+    bool plain = false;                                   // ref * scale is small enough for that
     __device__ __forceinline__ explicit ExpSum(double s) : scale(s) {}
+    __device__ __forceinline__ void set(float r) {
+        ref = r;
+        shift = rint(-static_cast<double>(ref) * scale);
+        plain = fabs(shift) < 3.0e7;                      // floor and ceiling are then off by 4 at most, as places
+    }
+    __device__ __forceinline__ double place(double x) const { return plain ? fma(x, scale, shift) : (x - static_cast<double>(ref)) * scale; }
     __device__ __forceinline__ void refer(float most) {
         // the same in all lanes, and known to be
-        ref = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(most)));
-        shift = -static_cast<double>(ref) * scale;
-        plain = __builtin_amdgcn_readfirstlane(fabs(shift) < 3.0e7) != 0;          // x scale + shift is then off by 4e-9 / 256 at most
+        set(__int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(most))));
+        plain = __builtin_amdgcn_readfirstlane(plain) != 0;
         floor = static_cast<float>(static_cast<double>(ref) + static_cast<double>(kLowest) / scale);
         ceiling = static_cast<float>(static_cast<double>(ref) + static_cast<double>(kHighest) / scale);
     }
-    // the sum as one of a reference `to`, not below ref
+    // the sum as one of exp((x - to) / T), `to` not below ref
     __device__ __forceinline__ double rebased(float to, const double* tab) const {
-        const double y = fmax((static_cast<double>(ref) - static_cast<double>(to)) * scale, static_cast<double>(kLowest));
+        const double y = fmax(-place(static_cast<double>(to)), static_cast<double>(kLowest));
         return ref > kNone ? sum * exp2_256_end(exp2_256_begin(y, tab), 0.0) : 0.0;
     }
     // from here on entries up to `most` (this lane's) come
@@ -214,6 +228,7 @@ struct ExpSum {
             most = wave_max_f(most);
             sum = rebased(most, tab);
             refer(most);
+            sum *= exp2_256_end(exp2_256_begin(place(static_cast<double>(ref)), tab), 0.0);
         }
     }
     // kEight entries per lane.  A NaN makes the sum NaN.
@@ -223,25 +238,25 @@ struct ExpSum {
 #pragma unroll
         for (int i = 1; i < kEight; ++i) least = fminf(least, x[i]);
         if (plain && !__any(least < floor)) {
+            const double shift_magic = shift + kExpMagic;
 #pragma unroll
             for (int i0 = 0; i0 < kEight; i0 += 4) {                              // four table entries on their way: eight would spill
                 ExpPart e[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) e[i] = exp2_256_begin(fma(static_cast<double>(x[i0 + i]), scale, shift), tab);
+                for (int i = 0; i < 4; ++i) e[i] = exp2_256_begin(static_cast<double>(x[i0 + i]), scale, shift_magic, tab);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sum = exp2_256_end(e[i], sum);
                 __builtin_amdgcn_sched_barrier(0);
             }
         } else {
-            // masked entries, lowest values, tiny temperatures: the difference first, which is exact
-            const double r = static_cast<double>(ref);
+            // masked entries, lowest values, tiny temperatures
 #pragma unroll 1
             for (int i = 0; i < kEight; ++i) {
                 float v = x[0];
 #pragma unroll
                 for (int j = 1; j < kEight; ++j) v = i == j ? x[j] : v;
-                const double upto = exp2_256_end(exp2_256_begin(fmax((static_cast<double>(v) - r) * scale, static_cast<double>(kLowest)), tab), sum);
+                const double upto = exp2_256_end(exp2_256_begin(fmax(place(static_cast<double>(v)), static_cast<double>(kLowest)), tab), sum);
                 sum = v == v ? upto : static_cast<double>(v);
             }
         }

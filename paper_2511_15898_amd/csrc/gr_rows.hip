@@ -353,7 +353,7 @@ __global__ __launch_bounds__(kThreads, SUM && !PROBS ? 4 : 5) void rows_kernel(c
         float ref = mine.es.ref;
         double sum = L.red[tid];
         if (kExp) {
-            mine.es.ref = L.edge[tid]; mine.es.sum = sum;
+            mine.es.set(L.edge[tid]); mine.es.sum = sum;
             ref = fmaxf(fmaxf(L.edge[0], L.edge[1]), fmaxf(L.edge[2], L.edge[3]));
             sum = mine.es.rebased(ref, L.tab);
         }
@@ -442,7 +442,7 @@ __device__ __forceinline__ PieceMass piece_mass(const RowChunks<T>& x, int piece
                 for (int j = 0; j < ExpSum::kEight; ++j) v[j] = Packed<T>::get(r[l + j / N], j % N);
                 es.add(v, tab);
             }
-            sum = es.sum;                                 // NaN if an entry is
+            sum = es.rebased(ref, tab);                   // NaN if an entry is
         } else {
             // nothing but masked entries and NaN, which the maximum passes over
 #pragma unroll
