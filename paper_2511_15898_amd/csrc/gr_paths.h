@@ -126,6 +126,8 @@ __device__ __forceinline__ float wave_max_f(float v) {
     return fmaxf(fmaxf(__int_as_float(__builtin_amdgcn_readlane(b, 0)), __int_as_float(__builtin_amdgcn_readlane(b, 16))),
                  fmaxf(__int_as_float(__builtin_amdgcn_readlane(b, 32)), __int_as_float(__builtin_amdgcn_readlane(b, 48))));
 }
+template <int CTRL>
+__device__ __forceinline__ float dpp_move_f(float v) { return __int_as_float(dpp_move<CTRL>(__float_as_int(v))); }
 __device__ __forceinline__ float wave_min_f(float v) { return -wave_max_f(-v); }
 
 // A row as 16-byte chunks at 16-byte boundaries, wherever it begins: chunk c holds elements [c N - lead, c N - lead + N).  Chunks that reach
@@ -292,6 +294,18 @@ __device__ __forceinline__ float bin_edge(float lo, float hi, int from) {
     return edge > lo ? edge : lo;                         // NaN, too: lo
 }
 
+// The smallest and the largest of what the waves left in `edge`: with many waves a lane to a wave.
+template <int NW>
+__device__ __forceinline__ void join_edges(const float* edge, float& lo, float& hi) {
+    if (NW <= 4) {
+#pragma unroll
+        for (int w = 0; w < NW; ++w) { lo = fminf(lo, edge[w]); hi = fmaxf(hi, edge[NW + w]); }
+    } else {
+        const int at = threadIdx.x & (NW - 1);
+        lo = wave_min_f(edge[at]); hi = wave_max_f(edge[NW + at]);
+    }
+}
+
 // Of c > k keys in LDS the largest ones, moved to its begin: at least k, at most `limit`; all threads call it.  Returns how many;
 // `reach`: a value that at least k of all keys' entries reach.
 // The keys go into 256 bins, linear over their range (entries are spread smoothly there: one round where digits of the bit pattern take three), and the
@@ -315,8 +329,7 @@ __device__ __forceinline__ int thin_keys(unsigned long long* keys, int c, int k,
     if (tid < 256) hist[tid] = 0;
     if (tid == 0) *count = 0;
     __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kNW; ++w) { lo = fminf(lo, edge[w]); hi = fmaxf(hi, edge[kNW + w]); }
+    join_edges<kNW>(edge, lo, hi);
     const float per = 255.f / (hi - lo);                  // infinite or 0 where all are equal, or some lie beyond float32 apart: the bins still rise with the entry
     const auto bin = [&](unsigned long long key) { return static_cast<int>(fminf(fmaxf((value(key) - lo) * per, 0.f), 255.f)); };   // NaN: 0
 #pragma unroll

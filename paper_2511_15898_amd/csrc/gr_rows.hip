@@ -69,37 +69,24 @@ __device__ __forceinline__ unsigned long long stretch_kth_largest(KeyAt key_at, 
 // largest of them.  With 8192 entries to a tile 9 reach it for k = 8, 136 for k = 128, 290 for k = 256.  First a bound from below: of 64 (128, 256) groups of threads, k at
 // least, the smallest of the groups' largest.  Then 256 linear bins from there to the largest entry.  All threads call it.
 template <int NT>
-__device__ __forceinline__ float find_threshold(const float* top, int k, int* hist, float* group_max, float* edge) {
+__device__ __forceinline__ float find_threshold(const float* top, int k, int* hist, float* edge) {
     constexpr int kNW = NT / 64;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     float most = top[0];
 #pragma unroll
     for (int l = 1; l < kLoads; ++l) most = fmaxf(most, top[l]);
-    float hi = wave_max_f(most);
+    // the largest of 2, 4, 8, 16 adjacent lanes, one of them the groups
+    const float of2 = fmaxf(most, dpp_move_f<kDppXor1>(most)), of4 = fmaxf(of2, dpp_move_f<kDppXor2>(of2)), of8 = fmaxf(of4, dpp_move_f<kDppHalfMirror>(of4));
+    const float of16 = fmaxf(of8, dpp_move_f<kDppMirror>(of8));
+    const float of[5] = {most, of2, of4, of8, of16};
+    constexpr int kOf256 = NT == 1024 ? 2 : (NT == 512 ? 1 : 0);                 // log2 of a group's lanes
+    const float group = k <= 64 ? of[kOf256 + 2] : (k <= 128 ? of[kOf256 + 1] : of[kOf256]);
+    float hi = wave_max_f(of16), lo = wave_min_f(group);
     __syncthreads();                                      // whoever reads what an earlier call left is done
     if (tid < 256) hist[tid] = 0;
-    if (lane == 0) edge[wave] = hi;
-    group_max[tid] = most;
+    if (lane == 0) { edge[wave] = lo; edge[kNW + wave] = hi; }
     __syncthreads();
-    // group g: the threads whose number is g modulo 64 (128, 256); a lane looks after groups lane, lane + 64, ..
-    float lo;
-    const auto bound = [&](auto groups) {
-        constexpr int G = decltype(groups)::value;
-        float least = __builtin_inff();
-#pragma unroll
-        for (int q = 0; q < G; q += 64) {
-            float m = kNone;
-#pragma unroll
-            for (int j = 0; j < NT; j += G) m = fmaxf(m, group_max[lane + q + j]);
-            least = fminf(least, m);
-        }
-        lo = wave_min_f(least);
-    };
-    if (k <= 64) bound(std::integral_constant<int, 64>{});
-    else if (k <= 128) bound(std::integral_constant<int, 128>{});
-    else bound(std::integral_constant<int, 256>{});
-#pragma unroll
-    for (int w = 0; w < kNW; ++w) hi = fmaxf(hi, edge[w]);
+    join_edges<kNW>(edge, lo, hi);
     if (!(lo > kNone)) return kNone;                      // the same for all threads
     const float per = 255.f / (hi - lo);
 #pragma unroll
@@ -134,7 +121,7 @@ struct ScanLds {
     uint4 list[kListCap<NT>];
     int list_chunk[kListCap<NT>];
     int hist[256], pick[4], count, listed[NT / 64];
-    float group_max[NT], edge[2 * (NT / 64)];
+    float edge[2 * (NT / 64)];
     double red[NT / 64], tab[EXP ? kExpEntries : 1];
 };
 // What a thread has of a slice behind a scan: how many keys lie in LDS (the same for all), whether it met a bad entry, its part of the sum (with its wave's reference).
@@ -185,9 +172,8 @@ __device__ __forceinline__ Scanned scan_slice(ScanLds<EXP, NT>& L, const Rows<T>
         if (lane == 0) listed[wave] = mine_listed;
         mine_listed = 0;
         __syncthreads();
-        int n[kNW], upto_wave[kNW], all = 0;
-#pragma unroll
-        for (int w = 0; w < kNW; ++w) { n[w] = listed[w]; over = over || n[w] > kWaveList<NT>; all += min(n[w], kWaveList<NT>); upto_wave[w] = all; }
+        const int n = lane < kNW ? listed[lane] : 0, upto_wave = wave_scan_i(min(n, kWaveList<NT>)), all = __builtin_amdgcn_readlane(upto_wave, 63);
+        over = over || __any(n > kWaveList<NT>);
 #pragma unroll
         for (int r = 0; r < kListCap<NT> / NT; ++r) {
             // the i-th chunk of the waves' shares one after the other
@@ -196,7 +182,10 @@ __device__ __forceinline__ Scanned scan_slice(ScanLds<EXP, NT>& L, const Rows<T>
             if (!__any(have)) break;
             int i = i0;
 #pragma unroll
-            for (int w = 1; w < kNW; ++w) if (i0 >= upto_wave[w - 1]) i = w * kWaveList<NT> + i0 - upto_wave[w - 1];
+            for (int w = 1; w < kNW; ++w) {
+                const int before = __builtin_amdgcn_readlane(upto_wave, w - 1);
+                if (i0 >= before) i = w * kWaveList<NT> + i0 - before;
+            }
             const uint4 raw = have ? list[i] : make_uint4(0u, 0u, 0u, 0u);
             const int chunk = have ? list_chunk[i] : 0;
             unsigned mask = 0u;
@@ -275,7 +264,7 @@ __device__ __forceinline__ Scanned scan_slice(ScanLds<EXP, NT>& L, const Rows<T>
                     es.add(v, tab);
                 }
         }
-        if (theta == kNone) theta = find_threshold<NT>(top, k, hist, L.group_max, edge);
+        if (theta == kNone) theta = find_threshold<NT>(top, k, hist, edge);
         unsigned long long hit[kLoads];
         int hits = 0;
 #pragma unroll
@@ -372,21 +361,23 @@ template <typename T, bool PROBS, int NT>
 __global__ __launch_bounds__(NT) void draft_rows_kernel(const Rows<T> in, int k, double tail_mass, const DraftOut out) {
     __shared__ union { ScanLds<false, NT> scan; DraftLds<kRowCap<NT>, NT> draft; } L;       // the keys are the first of both
     static_assert(offsetof(decltype(L.scan), keys) == 0 && offsetof(decltype(L.draft), keys) == 0 && sizeof(L.scan.keys) == sizeof(L.draft.keys));
-    __shared__ double q_wave[NT / 64];
-    __shared__ int bad_wave[NT / 64];
+    __shared__ double q_wave[PROBS ? NT / 64 : 1];
+    __shared__ int any_bad;
     const int tid = threadIdx.x, lane = tid & 63, row = blockIdx.x;
+    if (tid == 0) any_bad = 0;
     const RowChunks<T> x(in.row(row), in.V);
     const Uniforms<NT> uniforms(out, row);
     const float t = PROBS ? 1.f : in.temperature_of(row);
     const Scanned mine = scan_slice<T, PROBS, false, NT>(L.scan, in, row, x, 0, x.chunks, k);
-    const double q_mine = PROBS ? wave_sum(mine.total) : 0.0;
-    const bool bad_mine = __any(mine.bad != 0);
-    if (lane == 0) { q_wave[tid >> 6] = q_mine; bad_wave[tid >> 6] = bad_mine; }
+    if (PROBS) {
+        const double q_mine = wave_sum(mine.total);
+        if (lane == 0) q_wave[tid >> 6] = q_mine;
+    }
+    if (mine.bad) any_bad = 1;                            // cleared before the scan, which has barriers
     __syncthreads();
     double q_total = 0.0, inv_temp = 1.0;
-    bool bad = mine.found == 0;
-#pragma unroll
-    for (int w = 0; w < NT / 64; ++w) { q_total += q_wave[w]; bad = bad || bad_wave[w] != 0; }
+    if (PROBS) q_total = wave_sum(lane < NT / 64 ? q_wave[lane] : 0.0);
+    bool bad = mine.found == 0 || any_bad != 0;
     if (PROBS) bad = bad || !(fabs(q_total - 1.0) <= 1e-3);
     else if (!(t > 0.f) || !(t <= 3.0e38f)) bad = true;
     else inv_temp = 1.0 / static_cast<double>(t);
