@@ -2,9 +2,10 @@
 // where they are asked for, the sum of the row (probabilities) or of its exponentials (logits); and the sums of a row by pieces.
 // It stands behind the drafts' draw (gr_draft.hip) and the beams' selection (gr_beam.hip).
 //
-// Bound: HBM, one read of the row.  Arithmetic per element: about 5 instructions for a selection alone, about 20 with a float64 exponential
-// (float64 runs at the rate of unpacked float32 here), 0.83 us for a million elements and instruction on 32.8 million elements: for 16-bit
-// rows the exponentials and the read take about the same time, so both have to overlap.
+// Bound: HBM, one read of the row, where only the largest are asked for (about 5 instructions per element).  With the exponentials, in float64, it is about 20, 12 of them in the
+// innermost loop, and a rate of one instruction for 40 million million elements a second, which float64 has here as float32 has unpacked: 16.5 us for the 29.5 million bfloat16 logits
+// of 230 rows of 128256 that are read in 2.
+// Measured: those 27.5 us; 640 rows of 128256 in float32 81 us (4.0 TB/s); one row of 32000 7.7 us; without sums 256 rows of 128256 in bfloat16, k = 128, 20.6 us (3.2 TB/s).
 #include <algorithm>
 
 #include "gr_draft.h"
@@ -105,16 +106,17 @@ __device__ __forceinline__ float find_threshold(const float* top, int k, int* hi
     return bin_edge(lo, hi, from);
 }
 
-// grid = (splits * rows), 256 threads.  Workgroup s of a row reads chunks [s * per, (s + 1) * per) of its row, tiles of 256 * kLoads chunks, the next
+// rows_kernel: grid = (splits * rows), 256 threads.  Workgroup s of a row reads chunks [s * per, (s + 1) * per) of its row, tiles of 256 * kLoads chunks, the next
 // tile's loads on their way while the present one is worked on, and no barrier between tiles but for the threshold of the first.
 // The k largest: a chunk whose largest entry reaches the threshold goes, as it was loaded, to a list in LDS; the few on it are taken apart together at
-// the end (in the order of tiles every one would cost all lanes of its wave the test of every entry: 81 us where this takes %ROWS%).
+// the end (in the order of tiles every one would cost all lanes of its wave the test of every entry: 55 us where this takes 21, 256 rows of 128256 in bfloat16).
 // Keys are 64 bits (entry, ~id).  After `refresh` tiles the list is worked off and the threshold rises to about the k-th key.
 // A slice leaves at least its k largest, up to `limit` candidates.
 // SUM: PROBS: the float64 sum of the slice.  Logits: the sum of exp((x - ref) / T) in float64, per wave with its own reference, joined at the end.  (The hardware's float32
-// exponential, with the listed chunks in float64, was measured: %F32%, but sums good to 2e-8 only, which depend on how a row is cut.)
+// exponential, with the listed chunks in float64, took 22 us for 230 rows and 72 for 640 where this takes 27.5 and 81, but sums are good to 2e-8 only then, and beams closer than that
+// change places.)
 // Rows of beams that are not in use or finished are not read (Rows::skip).
-// Four waves to a SIMD with the exponentials: for a fifth their loop spills (32 us become 37, 89 become 114).
+// Four waves to a SIMD with the exponentials: for a fifth their loop spills (32 us became 37, 89 became 114).
 template <bool EXP, int NT>
 struct ScanLds {
     unsigned long long keys[kRowCap<NT>];
@@ -357,6 +359,8 @@ __global__ __launch_bounds__(kThreads, SUM && !PROBS ? 4 : 5) void rows_kernel(c
 }
 
 // The drafts of rows that one workgroup each reads: grid = (rows), NT threads.  No slices to join, so one launch does, and the candidates never leave LDS.
+// Bound: for one row a chain of dependent steps, 9.8 us for 32000 float32 logits, k = 64, of them 1.7 until the first tile has come, 1.9 for its threshold, 1.1 for the second tile, 1.7
+// to take the list apart, 1.4 to put 129 candidates in order, 0.8 to put 64 in order by id, 0.6 for the draws.  For 256 rows of 128256 in bfloat16 23 us, of which the read takes 10.
 template <typename T, bool PROBS, int NT>
 __global__ __launch_bounds__(NT) void draft_rows_kernel(const Rows<T> in, int k, double tail_mass, const DraftOut out) {
     __shared__ union { ScanLds<false, NT> scan; DraftLds<kRowCap<NT>, NT> draft; } L;       // the keys are the first of both
@@ -451,7 +455,7 @@ __device__ __forceinline__ double scale_of(const Rows<T>& in, int row) {
     return (temp > 0.f) && (temp <= 3.0e38f) ? kPerTemp / static_cast<double>(temp) : 0.0;
 }
 
-// The sums of a row by pieces, a wave to a piece.  grid = (pieces / 4 * rows).
+// The sums of a row by pieces, a wave to a piece.  grid = (pieces / 4 * rows).  Bound: HBM (probabilities) or the exponentials; 203 rows of 50021 probabilities 8.8 us (4.6 TB/s).
 template <typename T, bool PROBS>
 __global__ __launch_bounds__(kThreads) void masses_kernel(const Rows<T> in, int pieces, int stride, double* __restrict__ mass, float* __restrict__ refs) {
     __shared__ double tab[PROBS ? 1 : kExpEntries];
@@ -467,6 +471,7 @@ __global__ __launch_bounds__(kThreads) void masses_kernel(const Rows<T> in, int 
 }
 
 // Sums and draws of rows that one workgroup each reads, in one launch; the sums by pieces stay in LDS.  grid = (rows), NT threads.
+// Bound: HBM.  203 rows of 50021 probabilities, 16 draws each: 12.4 us (3.3 TB/s), 10.5 where the rows lie in the last cache.
 template <typename T, bool PROBS, int NT>
 __global__ __launch_bounds__(NT) void draft_whole_rows_kernel(const Rows<T> in, int pieces, const DraftOut out) {
     __shared__ double tab[PROBS ? 1 : kExpEntries], mass[kLdsPieces];
