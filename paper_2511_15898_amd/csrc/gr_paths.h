@@ -287,6 +287,13 @@ __device__ __forceinline__ unsigned long long cut_keys(unsigned long long* keys,
 }
 
 
+// Entries as they are counted in linear bins: logits as they are, probabilities by their bit pattern, about their logarithm (next to one of 0.9 the others would share a bin).  Rises with
+// the entry; no entry, a negative one or NaN: -inf.  unbinned: a value not above those whose place is `t` or more.
+template <bool PROBS>
+__device__ __forceinline__ float binned(float v) { return !PROBS ? v : (v >= 0.f ? static_cast<float>(__float_as_int(v)) : kNone); }
+template <bool PROBS>
+__device__ __forceinline__ float unbinned(float t) { return !PROBS || t == kNone ? t : __int_as_float(max(0, static_cast<int>(t) - 64)); }   // patterns are rounded to 24 bits
+
 // Not above any entry of bin `from` and those behind it, of 256 linear bins from lo to hi: the bin's lower edge, lowered by more than its roundings (a few 2^-24 of
 // either addend); not below lo.
 __device__ __forceinline__ float bin_edge(float lo, float hi, int from) {
@@ -316,7 +323,7 @@ __device__ __forceinline__ int thin_keys(unsigned long long* keys, int c, int k,
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     constexpr int kEach = CAP / NT;
     unsigned long long mine[kEach];
-    const auto value = [](unsigned long long key) { return PROBS ? key_q(key) : key_logit(key); };
+    const auto value = [](unsigned long long key) { return PROBS ? binned<true>(key_q(key)) : key_logit(key); };
     float lo = __builtin_inff(), hi = kNone;
 #pragma unroll
     for (int r = 0; r < kEach; ++r) {
@@ -349,13 +356,13 @@ __device__ __forceinline__ int thin_keys(unsigned long long* keys, int c, int k,
     if (left > limit) {
         __syncthreads();
         const unsigned long long kth = cut_keys<CAP, NT>(keys, count, c, k, hist, pick);
-        if (reach) *reach = value(kth);
+        if (reach) *reach = unbinned<PROBS>(value(kth));
         return k;
     }
 #pragma unroll
     for (int r = 0; r < kEach; ++r) if (mine[r] != 0ull && bin(mine[r]) >= from) keys[atomicAdd(count, 1)] = mine[r];
     __syncthreads();
-    if (reach) *reach = bin_edge(lo, hi, from);
+    if (reach) *reach = unbinned<PROBS>(bin_edge(lo, hi, from));
     return left;
 }
 

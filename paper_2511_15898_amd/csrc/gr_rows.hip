@@ -66,29 +66,30 @@ __device__ __forceinline__ unsigned long long stretch_kth_largest(KeyAt key_at, 
     return prefix;
 }
 
-// A threshold that at least k of the entries reach (-inf: there are too few), from the largest entries `top` of the threads' chunks (kLoads each, different entries): about the k-th
-// largest of them.  With 8192 entries to a tile 9 reach it for k = 8, 136 for k = 128, 290 for k = 256.  First a bound from below: of 64 (128, 256) groups of threads, k at
-// least, the smallest of the groups' largest.  Then 256 linear bins from there to the largest entry.  All threads call it.
-template <int NT>
-__device__ __forceinline__ float find_threshold(const float* top, int k, int* hist, float* edge) {
+// A threshold that at least k of the entries reach (-inf: none was found), from the largest entries `top` of the threads' chunks (kLoads each, different entries; -inf: none), of which
+// `threads` have some: about the k-th largest of them.  With 8192 entries to a tile 9 reach it for k = 8, 136 for k = 128, 290 for k = 256.  First a bound from below: of k groups of
+// adjacent lanes at least the smallest of the groups' largest.  Then 256 linear bins from there to the largest entry.  All threads call it.
+template <bool PROBS, int NT>
+__device__ __forceinline__ float find_threshold(const float* tops, int threads, int k, int* hist, float* edge) {
     constexpr int kNW = NT / 64;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    float most = top[0];
+    float top[kLoads], most = kNone;
 #pragma unroll
-    for (int l = 1; l < kLoads; ++l) most = fmaxf(most, top[l]);
-    // the largest of 2, 4, 8, 16 adjacent lanes, one of them the groups
+    for (int l = 0; l < kLoads; ++l) { top[l] = binned<PROBS>(tops[l]); most = fmaxf(most, top[l]); }
+    // the largest of 2, 4, 8, 16 lanes; groups as large as leave k of them, where nothing is masked
     const float of2 = fmaxf(most, dpp_move_f<kDppXor1>(most)), of4 = fmaxf(of2, dpp_move_f<kDppXor2>(of2)), of8 = fmaxf(of4, dpp_move_f<kDppHalfMirror>(of4));
     const float of16 = fmaxf(of8, dpp_move_f<kDppMirror>(of8));
-    const float of[5] = {most, of2, of4, of8, of16};
-    constexpr int kOf256 = NT == 1024 ? 2 : (NT == 512 ? 1 : 0);                 // log2 of a group's lanes
-    const float group = k <= 64 ? of[kOf256 + 2] : (k <= 128 ? of[kOf256 + 1] : of[kOf256]);
-    float hi = wave_max_f(of16), lo = wave_min_f(group);
+    const int size = threads >= 16 * k ? 16 : (threads >= 8 * k ? 8 : (threads >= 4 * k ? 4 : (threads >= 2 * k ? 2 : 1)));
+    const float group = size == 16 ? of16 : (size == 8 ? of8 : (size == 4 ? of4 : (size == 2 ? of2 : most)));
+    const bool any = group > kNone;
+    float hi = wave_max_f(of16), lo = wave_min_f(any ? group : __builtin_inff()), lanes = static_cast<float>(__popcll(__ballot(any)));
     __syncthreads();                                      // whoever reads what an earlier call left is done
     if (tid < 256) hist[tid] = 0;
-    if (lane == 0) { edge[wave] = lo; edge[kNW + wave] = hi; }
+    if (lane == 0) { edge[wave] = lo; edge[kNW + wave] = hi; edge[2 * kNW + wave] = lanes; }
     __syncthreads();
     join_edges<kNW>(edge, lo, hi);
-    if (!(lo > kNone)) return kNone;                      // the same for all threads
+    lanes = wave_sum_f32(lane < kNW ? edge[2 * kNW + lane] : 0.f);
+    if (lanes < static_cast<float>(size * k)) return kNone;                      // the same for all threads
     const float per = 255.f / (hi - lo);
 #pragma unroll
     for (int l = 0; l < kLoads; ++l) if (top[l] >= lo) atomicAdd(&hist[static_cast<int>(fminf(fmaxf((top[l] - lo) * per, 0.f), 255.f))], 1);
@@ -103,7 +104,7 @@ __device__ __forceinline__ float find_threshold(const float* top, int k, int* hi
 #pragma unroll
         for (int j = 0; j < 4; ++j) { above += in[j]; if (from < 0 && above >= k) from = 255 - 4 * lane - j; }
     from = __builtin_amdgcn_readlane(from, __ffsll(static_cast<unsigned long long>(__ballot(mine_is))) - 1);
-    return bin_edge(lo, hi, from);
+    return unbinned<PROBS>(bin_edge(lo, hi, from));
 }
 
 // rows_kernel: grid = (splits * rows), 256 threads.  Workgroup s of a row reads chunks [s * per, (s + 1) * per) of its row, tiles of 256 * kLoads chunks, the next
@@ -123,7 +124,7 @@ struct ScanLds {
     uint4 list[kListCap<NT>];
     int list_chunk[kListCap<NT>];
     int hist[256], pick[4], count, listed[NT / 64];
-    float edge[2 * (NT / 64)];
+    float edge[3 * (NT / 64)];
     double red[NT / 64], tab[EXP ? kExpEntries : 1];
 };
 // What a thread has of a slice behind a scan: how many keys lie in LDS (the same for all), whether it met a bad entry, its part of the sum (with its wave's reference).
@@ -266,7 +267,7 @@ __device__ __forceinline__ Scanned scan_slice(ScanLds<EXP, NT>& L, const Rows<T>
                     es.add(v, tab);
                 }
         }
-        if (theta == kNone) theta = find_threshold<NT>(top, k, hist, edge);
+        if (theta == kNone) theta = find_threshold<PROBS, NT>(top, min(NT, c_end - c0), k, hist, edge);
         unsigned long long hit[kLoads];
         int hits = 0;
 #pragma unroll
