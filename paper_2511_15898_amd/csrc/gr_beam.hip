@@ -10,7 +10,6 @@ namespace {
 constexpr int kMergeThreads = 512, kMergeWaves = kMergeThreads / 64, kMergeCap = 1024;
 static_assert(GR_MAX_BEAMS * kMaxSplits <= 2048, "beam_of");
 constexpr int kMaxLists = GR_MAX_BEAMS * kMaxSplits;
-constexpr int kHeldLists = 8;                             // lists of a wave whose keys are on their way at once
 constexpr int kBatchKeys = kMergeWaves * GR_MAX_BEAMS;    // a wave to a slice's list, at most GR_MAX_BEAMS keys each
 static_assert(kMergeCap >= GR_MAX_BEAMS + kBatchKeys, "a batch always has room behind the best ones");
 constexpr double kNoScore = -__builtin_inf();
@@ -81,7 +80,9 @@ __device__ __forceinline__ void keep_best(MergeLds& L, int c, int M) {
 // M-th best, from groups of threads, leaves some dozens, which are put in order by counting.
 // Bound: a chain of steps behind one read.  What the slices left lies in other chips' L2, a microsecond away, so counts, sums and keys are all asked for at the
 // beginning, keys before it is known how many there are (each list after the other took 25 us for 64 lists).
-// 7.8 us for one sequence of 4 beams in 8 slices each, M = 4; 9.9 us for 32 sequences of 8 beams in 4 slices, M = 16, and for 64 of 10 in 3, M = 20.
+// 8.0 us for one sequence of 4 beams in 8 slices each, M = 4; 8.8 us for 32 sequences of 8 beams in 4 slices, M = 16, and for 64 of 10 in 3, M = 20.
+// HELD: lists of a wave whose keys are on their way at once, and stay in registers if there are no more.
+template <int HELD>
 __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(const Rows<float> in, int K, int M, int eos, int splits, int inverse, const RowParts parts, const BeamOut out) {
     __shared__ MergeLds L;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), seq = blockIdx.x;
@@ -93,9 +94,9 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(const Rows<fl
         const int b = beam_of(list), i = place(list);
         return list < lists && i < most ? parts.cand[static_cast<size_t>(row0 + b) * kSelCap + (list - b * splits) * room + i] : 0ull;
     };
-    unsigned long long held[kHeldLists];                  // of lists wave, wave + 8, ..
+    unsigned long long held[HELD];                  // of lists wave, wave + 8, ..
 #pragma unroll
-    for (int u = 0; u < kHeldLists; ++u) held[u] = load_key(wave + u * kMergeWaves);
+    for (int u = 0; u < HELD; ++u) held[u] = load_key(wave + u * kMergeWaves);
     const float temp = in.temperature ? in.temperature[seq] : 1.f;
     const double inv_temp = 1.0 / static_cast<double>(temp);
     // a wave to a beam, a lane to a slice; of two beams everything is asked for at once
@@ -141,21 +142,23 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(const Rows<fl
         if (list >= lists || place(list) >= L.lists[list]) return false;
         const int b = beam_of(list);
         value = L.score[b] + ((static_cast<double>(key_logit(key)) - L.top[b]) * inv_temp - L.log_sum[b]);
+        // to a multiple of 2^-35, a seventh of what the sums may be off by: sums of equal rows that were added up in another order meet again, so equal beams tie (but for one in thousands)
+        value = rint(value * 0x1p35) * 0x1p-35;
         return true;
     };
-    // Calls use(list, key, value) for every candidate.  Up to 64 lists stay in registers, keys and scores.
-    double scores_held[kHeldLists];
-    const bool all_held = lists <= kHeldLists * kMergeWaves;
+    // Calls use(list, key, value) for every candidate.
+    double scores_held[HELD];
+    const bool all_held = lists <= HELD * kMergeWaves;
     const auto each = [&](bool again, auto&& use) {
-        for (int l0 = 0; l0 < lists; l0 += kHeldLists * kMergeWaves) {
+        for (int l0 = 0; l0 < lists; l0 += HELD * kMergeWaves) {
             if (!all_held)
 #pragma unroll
-                for (int u = 0; u < kHeldLists; ++u) held[u] = load_key(l0 + wave + u * kMergeWaves);
+                for (int u = 0; u < HELD; ++u) held[u] = load_key(l0 + wave + u * kMergeWaves);
             if (!all_held || !again)
 #pragma unroll
-                for (int u = 0; u < kHeldLists; ++u) if (!candidate(l0 + wave + u * kMergeWaves, held[u], scores_held[u])) scores_held[u] = kNoScore;
+                for (int u = 0; u < HELD; ++u) if (!candidate(l0 + wave + u * kMergeWaves, held[u], scores_held[u])) scores_held[u] = kNoScore;
 #pragma unroll
-            for (int u = 0; u < kHeldLists; ++u) if (scores_held[u] > kNoScore) use(l0 + wave + u * kMergeWaves, held[u], scores_held[u]);
+            for (int u = 0; u < HELD; ++u) if (scores_held[u] > kNoScore) use(l0 + wave + u * kMergeWaves, held[u], scores_held[u]);
         }
     };
     double mine = kNoScore;
@@ -347,7 +350,15 @@ __global__ __launch_bounds__(kThreads) void reorder_kernel(const ReorderParams r
 }  // namespace
 
 void launch_beam_merge(const RowSource& src, int S, int K, int M, int eos, RowSlices cut, const RowParts& in, const BeamOut& out, hipStream_t stream) {
-    hipLaunchKernelGGL(beam_merge_kernel, dim3(S), dim3(kMergeThreads), 0, stream, Rows<float>(src), K, M, eos, cut.splits, (65536 + cut.splits - 1) / cut.splits, in, out);
+    const auto run = [&](auto held) {
+        hipLaunchKernelGGL(beam_merge_kernel<decltype(held)::value>, dim3(S), dim3(kMergeThreads), 0, stream, Rows<float>(src), K, M, eos, cut.splits, (65536 + cut.splits - 1) / cut.splits, in, out);
+    };
+    // As many as there are: of 12 lists 7.8 us with 2, 8.5 with 8, 9.0 with 16; of 100 11.5 with 16, 15.4 with 8, which asks twice, each time for all.
+    const int lists = K * cut.splits;
+    if (lists <= 2 * kMergeWaves) run(std::integral_constant<int, 2>{});
+    else if (lists <= 4 * kMergeWaves) run(std::integral_constant<int, 4>{});
+    else if (lists <= 8 * kMergeWaves) run(std::integral_constant<int, 8>{});
+    else run(std::integral_constant<int, 16>{});
 }
 
 void launch_reorder(const ReorderParams& params, hipStream_t stream) {
