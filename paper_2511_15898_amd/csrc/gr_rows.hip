@@ -216,8 +216,8 @@ __device__ __forceinline__ Scanned scan_slice(ScanLds<EXP, NT>& L, const Rows<T>
     const int quarter = (c_end - c_first + 3) / 4;
     for (int c0 = c_first; c0 < c_end; c0 += kTileChunks) {
         if (kExp) {
-            // Arithmetic bounds this loop, and of the waves on a SIMD the oldest would run through first and leave the last alone, with nothing to cover its latencies (the workgroups of
-            // a compute unit ended after 16 to 32 us).  Those that are behind go first: all end together, 31.4 us become 28.4 (256 rows of 128256 in bfloat16), 86 become 82.
+            // Arithmetic bounds this loop, and of the waves on a SIMD the oldest goes first by itself, so that the last is left with nothing to cover its latencies.  Those that are behind go
+            // first: 31.4 us become 28.4 (256 rows of 128256 in bfloat16), 86 become 82 (640 in float32).
             const int gone = c0 - c_first;
             if (gone < quarter) __builtin_amdgcn_s_setprio(3);
             else if (gone < 2 * quarter) __builtin_amdgcn_s_setprio(2);
