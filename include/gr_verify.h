@@ -233,7 +233,8 @@ int gr_solve_logits_verify(gr_handle h, const float* target_logits, const float*
  * drafts      [B, n] int32 out.   status [B] int32 out: GR_ROW_OK, or GR_ROW_BAD (NaN or negative entry, a row sum further than 1e-3 from 1, no
  *             positive entry): the row's drafts are then -1.
  * Overwrites the handle's selection scratch: the policy of an earlier gr_solve is gone (gr_verify returns GR_ESTATE until the next gr_solve).
- * Neither allocates nor synchronises.  The same draws come out whatever rows stand beside a row, and from run to run.
+ * Neither allocates nor synchronises.  The same draws come out from run to run, and whatever rows stand beside a row (of a nucleus cut but for a row whose
+ * cut lies within float64 rounding of the next token).
  */
 int gr_draft(gr_handle h, const float* q, long long row_stride, int n, int k, const float* uniforms, int B, int V,
              int* drafts, int* status, void* hip_stream);
@@ -306,6 +307,7 @@ int gr_beam_reorder(void* state, const gr_state_layout* layout, const int* paren
  * slots       [slots_capacity] int64: for every new token, in order, table entry * block + place in the block (-1 where the entry is below 0); entries from
  *             starts[R] on are left as they are.
  * status      [R] int32.
+ * Blocks are not counted: one that two requests share (a common prompt) must be given back by one of them at most, and not while the other needs it.
  * lengths, new_lengths and free_count are only read, and the out arrays must be others: a decoding loop keeps two sets and swaps them.
  * 1 <= R <= GR_MAX_REQUESTS, R * width, pool and slots_capacity below 2^31.  No handle, no scratch; one launch; neither allocates nor synchronises.
  */

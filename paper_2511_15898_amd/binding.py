@@ -508,8 +508,8 @@ def gr_beam_reorder(state: torch.Tensor, parent: torch.Tensor, first: torch.Tens
 def gr_page_update(lengths: torch.Tensor, new_lengths: torch.Tensor, table: torch.Tensor, free_blocks: torch.Tensor, free_count: torch.Tensor,
                    block: int, slots: torch.Tensor, out=None, stream=None):
     """Block tables, slots and the free stack after lengths [R] -> new_lengths [R] (int32): table [R, width] int32, free_blocks [pool] int32 and slots [capacity]
-    int64 are updated, free_count [1] int32 is read.  Returns (lengths [R], free_count [1], starts [R + 1], status [R]), all int32; `out`: the same four
-    tensors to write to, others than the ones read."""
+    int64 are updated, free_count [1] int32 is read; blocks are not counted, so one that two requests share is given back by one of them at most.
+    Returns (lengths [R], free_count [1], starts [R + 1], status [R]), all int32; `out`: the same four tensors to write to, others than the ones read."""
     if lengths.dim() != 1 or table.dim() != 2 or free_blocks.dim() != 1 or slots.dim() != 1:
         raise TypeError("gr_page_update: lengths [R], table [R, width], free_blocks [pool], slots [capacity]")
     R, width = lengths.shape[0], table.shape[1]

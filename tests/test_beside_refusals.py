@@ -77,3 +77,24 @@ for i in range(launches):
     result["seen"].append([rc, {call}, solve(h, 4, 600, 3, 32), verify(h, 4)])
 """)
     assert r["seen"] and all(x == [EHIP, 0, 0, 0] for x in r["seen"]), r["seen"]
+
+
+@pytest.mark.parametrize("call, launches", [("draft(big, B=1, V=200000, stride=200000)", 2), ("draft(big, B=1, V=200000, stride=200000, k=0)", 2), ("draft_logits(big, B=1, V=200000, stride=200000, k=0)", 2),
+                                            ("draft(big, B=1, V=5000, stride=5000)", 1), ("draft(big, B=1, V=5000, stride=5000, k=0)", 1), ("draft(big, B=200, V=200000, stride=200000)", 1),
+                                            ("draft(big, B=200, V=200000, stride=200000, k=0)", 1), ("draft_logits(big, B=200, V=200000, stride=200000)", 1), ("select(big)", 2)])
+def test_launches_of_few_long_rows_and_of_others(recorded, call, launches):  # noqa: F811
+    """A failure of either launch is reported, and the next call is as ever."""
+    r = recorded(CALLS + f"""
+big = create(200, 200000, 32, 3)
+hip.recorded_clear()
+assert {call} == 0
+result["launches"] = len(log())
+result["seen"] = []
+for i in range(result["launches"]):
+    hip.recorded_clear()
+    hip.recorded_fail(b"launch", i)
+    rc = {call}
+    hip.recorded_clear()
+    result["seen"].append([rc, {call}])
+""")
+    assert r["launches"] == launches and all(x == [EHIP, 0] for x in r["seen"]), r
