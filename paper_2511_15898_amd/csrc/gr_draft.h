@@ -8,16 +8,6 @@ namespace gr {
 constexpr int kRanked = 512;                              // candidates put in order at once
 constexpr int kSupportRegs = kMaxSupport / 64;
 
-__device__ __forceinline__ double wave_scan_d(double v) {  // inclusive, all lanes active
-    v += dpp_shift<0x111, 0xF>(v, 0.0);
-    v += dpp_shift<0x112, 0xF>(v, 0.0);
-    v += dpp_shift<0x114, 0xF>(v, 0.0);
-    v += dpp_shift<0x118, 0xF>(v, 0.0);
-    v += dpp_shift<0x142, 0xA>(v, 0.0);
-    v += dpp_shift<0x143, 0xC>(v, 0.0);
-    return v;
-}
-
 // CAP: candidates, in `keys`.
 template <int CAP, int NT>
 struct DraftLds {

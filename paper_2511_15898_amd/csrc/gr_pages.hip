@@ -37,9 +37,9 @@ __global__ __launch_bounds__(kPageThreads) void pages_kernel(const PageParams pp
     extern __shared__ int lds[];
     const int R = pp.R;
     int* const starts = lds; int* const fresh = lds + R + 1; int* const freed = lds + 2 * (R + 1); int* const from = lds + 3 * (R + 1); int* const open = lds + 4 * (R + 1);
-    __shared__ long long wave_tokens[kPageWaves], wave_fresh[kPageWaves], wave_freed[kPageWaves];
+    __shared__ double wave_tokens[kPageWaves], wave_fresh[kPageWaves], wave_freed[kPageWaves];
     __shared__ unsigned long long got_tokens, got_fresh;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool first = blockIdx.x == 0;
     const int per = (R + kPageThreads - 1) / kPageThreads, r0 = min(R, tid * per), mine = min(R, r0 + per) - r0;
     const long long most = static_cast<long long>(pp.width) * pp.block;
@@ -64,21 +64,15 @@ __global__ __launch_bounds__(kPageThreads) void pages_kernel(const PageParams pp
                 if (OPEN && j < had) part[i] = pp.table[static_cast<long long>(r0 + i) * pp.width + j];
             } else give += had - has;
         }
-    // sums over the requests of the threads before
-    const auto scan = [&](long long v) {
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) { const long long w = __shfl_up(v, o); if (lane >= o) v += w; }
-        return v;
-    };
-    long long tokens_to = scan(tokens), need_to = scan(need), give_to = scan(give);
-    if (lane == 63) { wave_tokens[wave] = tokens_to; wave_fresh[wave] = need_to; wave_freed[wave] = give_to; }
+    // Sums over the requests of the threads before: 2^44 at most, which float64 holds.  All waves join the waves' sums, a lane to a wave.
+    const double tokens_in = wave_scan_d(static_cast<double>(tokens)), need_in = wave_scan_d(static_cast<double>(need)), give_in = wave_scan_d(static_cast<double>(give));
+    if (lane == 63) { wave_tokens[wave] = tokens_in; wave_fresh[wave] = need_in; wave_freed[wave] = give_in; }
     __syncthreads();
-    long long given = 0;
-#pragma unroll
-    for (int w = 0; w < kPageWaves; ++w) {
-        if (w < wave) { tokens_to += wave_tokens[w]; need_to += wave_fresh[w]; give_to += wave_freed[w]; }
-        given += wave_freed[w];
-    }
+    const bool is_wave = lane < kPageWaves;
+    const double tokens_up = wave_scan_d(is_wave ? wave_tokens[lane] : 0.0), need_up = wave_scan_d(is_wave ? wave_fresh[lane] : 0.0), give_up = wave_scan_d(is_wave ? wave_freed[lane] : 0.0);
+    const auto before = [&](double up) { return wave > 0 ? read_lane(up, wave - 1) : 0.0; };
+    const long long tokens_to = static_cast<long long>(tokens_in + before(tokens_up)), need_to = static_cast<long long>(need_in + before(need_up));
+    const long long give_to = static_cast<long long>(give_in + before(give_up)), given = static_cast<long long>(read_lane(give_up, 63));
     // Grants in order: the sums only rise, so from the first request that finds too little on, every growing one does, and what is granted are the
     // sums before that one.
     const long long have = count + given;

@@ -130,6 +130,17 @@ template <int CTRL>
 __device__ __forceinline__ float dpp_move_f(float v) { return __int_as_float(dpp_move<CTRL>(__float_as_int(v))); }
 __device__ __forceinline__ float wave_min_f(float v) { return -wave_max_f(-v); }
 
+__device__ __forceinline__ double wave_scan_d(double v) {  // inclusive, all lanes active
+    v += dpp_shift<0x111, 0xF>(v, 0.0);
+    v += dpp_shift<0x112, 0xF>(v, 0.0);
+    v += dpp_shift<0x114, 0xF>(v, 0.0);
+    v += dpp_shift<0x118, 0xF>(v, 0.0);
+    v += dpp_shift<0x142, 0xA>(v, 0.0);
+    v += dpp_shift<0x143, 0xC>(v, 0.0);
+    return v;
+}
+
+
 // A row as 16-byte chunks at 16-byte boundaries, wherever it begins: chunk c holds elements [c N - lead, c N - lead + N).  Chunks that reach
 // over an end of the row are read element by element, entries outside it are -inf.
 template <typename T>
