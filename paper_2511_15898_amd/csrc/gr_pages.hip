@@ -8,7 +8,7 @@ namespace gr {
 namespace {
 
 constexpr int kPageThreads = 1024, kPageWaves = kPageThreads / 64, kRun = 4;
-constexpr long long kMostInt = 0x7FFFFFFFll;
+constexpr double kMostTokens = 2147483648.0;
 
 // Division by a fixed block size: a shift where it is a power of two.
 struct BlockSize {
@@ -37,8 +37,9 @@ __global__ __launch_bounds__(kPageThreads) void pages_kernel(const PageParams pp
     extern __shared__ int lds[];
     const int R = pp.R;
     int* const starts = lds; int* const fresh = lds + R + 1; int* const freed = lds + 2 * (R + 1); int* const from = lds + 3 * (R + 1); int* const open = lds + 4 * (R + 1);
-    __shared__ double wave_tokens[kPageWaves], wave_fresh[kPageWaves], wave_freed[kPageWaves];
-    __shared__ unsigned long long got_tokens, got_fresh;
+    __shared__ double wave_tokens[kPageWaves];
+    __shared__ int wave_fresh[kPageWaves], wave_freed[kPageWaves];
+    __shared__ unsigned got_tokens, got_fresh;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const bool first = blockIdx.x == 0;
     const int per = (R + kPageThreads - 1) / kPageThreads, r0 = min(R, tid * per), mine = min(R, r0 + per) - r0;
@@ -49,8 +50,9 @@ __global__ __launch_bounds__(kPageThreads) void pages_kernel(const PageParams pp
     int old[kPerThread], now[kPerThread], part[kPerThread];
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) if (i < mine) { old[i] = pp.lengths[r0 + i]; now[i] = pp.new_lengths[r0 + i]; }
-    if (tid == 0) { got_tokens = ~0ull; got_fresh = ~0ull; }
-    long long tokens = 0, need = 0, give = 0;
+    if (tid == 0) { got_tokens = ~0u; got_fresh = ~0u; }
+    double tokens = 0.0;                                  // up to 2^44; blocks are at most R * width, below 2^31
+    int need = 0, give = 0;
     unsigned bad = 0u;
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i)
@@ -59,58 +61,62 @@ __global__ __launch_bounds__(kPageThreads) void pages_kernel(const PageParams pp
             if (old[i] < 0 || now[i] < 0 || old[i] > most || now[i] > most) { bad |= 1u << i; continue; }
             const int had = static_cast<int>(bs.up(old[i])), has = static_cast<int>(bs.up(now[i]));
             if (now[i] > old[i]) {
-                tokens += now[i] - old[i]; need += has - had;
+                tokens += static_cast<double>(now[i] - old[i]); need += has - had;
                 const int j = static_cast<int>(bs.div(old[i]));
                 if (OPEN && j < had) part[i] = pp.table[static_cast<long long>(r0 + i) * pp.width + j];
             } else give += had - has;
         }
-    // Sums over the requests of the threads before: 2^44 at most, which float64 holds.  All waves join the waves' sums, a lane to a wave.
-    const double tokens_in = wave_scan_d(static_cast<double>(tokens)), need_in = wave_scan_d(static_cast<double>(need)), give_in = wave_scan_d(static_cast<double>(give));
+    // Sums over the requests of the threads before.  All waves join the waves' sums, a lane to a wave.
+    const double tokens_in = wave_scan_d(tokens);
+    const int need_in = wave_scan_i(need), give_in = wave_scan_i(give);
     if (lane == 63) { wave_tokens[wave] = tokens_in; wave_fresh[wave] = need_in; wave_freed[wave] = give_in; }
     __syncthreads();
     const bool is_wave = lane < kPageWaves;
-    const double tokens_up = wave_scan_d(is_wave ? wave_tokens[lane] : 0.0), need_up = wave_scan_d(is_wave ? wave_fresh[lane] : 0.0), give_up = wave_scan_d(is_wave ? wave_freed[lane] : 0.0);
-    const auto before = [&](double up) { return wave > 0 ? read_lane(up, wave - 1) : 0.0; };
-    const long long tokens_to = static_cast<long long>(tokens_in + before(tokens_up)), need_to = static_cast<long long>(need_in + before(need_up));
-    const long long give_to = static_cast<long long>(give_in + before(give_up)), given = static_cast<long long>(read_lane(give_up, 63));
+    const double tokens_up = wave_scan_d(is_wave ? wave_tokens[lane] : 0.0);
+    const int need_up = wave_scan_i(is_wave ? wave_fresh[lane] : 0), give_up = wave_scan_i(is_wave ? wave_freed[lane] : 0), given = __builtin_amdgcn_readlane(give_up, 63);
+    const double tokens_to = tokens_in + (wave > 0 ? read_lane(tokens_up, wave - 1) : 0.0);
+    const int need_to = need_in + (wave > 0 ? __builtin_amdgcn_readlane(need_up, wave - 1) : 0), give_to = give_in + (wave > 0 ? __builtin_amdgcn_readlane(give_up, wave - 1) : 0);
     // Grants in order: the sums only rise, so from the first request that finds too little on, every growing one does, and what is granted are the
     // sums before that one.
-    const long long have = count + given;
-    long long at_tokens = tokens_to - tokens, at_need = need_to - need, at_give = give_to - give;
+    const unsigned have = static_cast<unsigned>(count) + static_cast<unsigned>(given), capacity = static_cast<unsigned>(pp.slots_capacity);
+    // tokens beyond 2^31 are beyond any capacity, and stay there: a request adds 2^31 at most
+    unsigned at_tokens = static_cast<unsigned>(fmin(tokens_to - tokens, kMostTokens));
+    int at_need = need_to - need, at_give = give_to - give;
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i)
         if (i < mine) {
             const int r = r0 + i;
-            starts[r] = static_cast<int>(min(at_tokens, kMostInt)); fresh[r] = static_cast<int>(min(at_need, kMostInt)); freed[r] = static_cast<int>(at_give);
+            starts[r] = static_cast<int>(min(at_tokens, 0x7FFFFFFFu)); fresh[r] = at_need; freed[r] = at_give;
             int status = GR_ROW_OK, length = now[i];
             from[r] = old[i];
             if (bad >> i & 1u) { status = GR_ROW_BAD; length = old[i]; }
             else if (now[i] > old[i]) {
-                const long long before_tokens = at_tokens, before_need = at_need;
-                at_tokens += now[i] - old[i];
+                const unsigned before_tokens = at_tokens;
+                const int before_need = at_need;
+                at_tokens = min(at_tokens, 0x7FFFFFFFu) + static_cast<unsigned>(now[i] - old[i]);
                 at_need += static_cast<int>(bs.up(now[i])) - static_cast<int>(bs.up(old[i]));
-                if (at_need > have || at_tokens > pp.slots_capacity) {
+                if (static_cast<unsigned>(at_need) > have || at_tokens > capacity) {
                     status = GR_ROW_NO_ROOM; length = old[i];
-                    atomicMin(&got_tokens, static_cast<unsigned long long>(before_tokens)); atomicMin(&got_fresh, static_cast<unsigned long long>(before_need));
+                    atomicMin(&got_tokens, before_tokens); atomicMin(&got_fresh, static_cast<unsigned>(before_need));
                 }
             } else { at_give += static_cast<int>(bs.up(old[i])) - static_cast<int>(bs.up(now[i])); from[r] = now[i]; }
             if (OPEN) open[r] = part[i];
             if (first) { pp.out_lengths[r] = length; pp.status[r] = status; }
         }
     if (tid == kPageThreads - 1) {
-        starts[R] = static_cast<int>(min(tokens_to, kMostInt)); fresh[R] = static_cast<int>(min(need_to, kMostInt)); freed[R] = static_cast<int>(given);
+        starts[R] = static_cast<int>(min(static_cast<unsigned>(fmin(tokens_to, kMostTokens)), 0x7FFFFFFFu)); fresh[R] = need_to; freed[R] = given;
     }
     __syncthreads();
-    const bool refused = got_tokens != ~0ull;
+    const bool refused = got_tokens != ~0u;
     if (refused) {                                        // the same for all threads
         const int t = static_cast<int>(got_tokens), f = static_cast<int>(got_fresh);
         for (int r = tid; r <= R; r += kPageThreads) { starts[r] = min(starts[r], t); fresh[r] = min(fresh[r], f); }
         __syncthreads();
     }
-    const int T = starts[R], fresh_all = fresh[R], freed_all = static_cast<int>(given);
+    const int T = starts[R], fresh_all = fresh[R], freed_all = given;
     if (first) {
         for (int r = tid; r <= R; r += kPageThreads) pp.starts[r] = starts[r];
-        if (tid == 0) *pp.out_free_count = static_cast<int>(min(have - fresh_all, static_cast<long long>(pp.pool)));
+        if (tid == 0) *pp.out_free_count = static_cast<int>(min(have - static_cast<unsigned>(fresh_all), static_cast<unsigned>(pp.pool)));
     }
 
     // the m-th released block, by request and place; the table's rows of shrinking requests are written by nobody

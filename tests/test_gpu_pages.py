@@ -184,3 +184,37 @@ def test_a_beam_search_over_pages(torch, gr):
         assert int(left) == pool and sorted(stack.cpu().tolist()) == list(range(pool))
     finally:
         gr.gr_destroy(h)
+
+
+@pytest.mark.parametrize("R", [6, 700, 8000])
+@pytest.mark.parametrize("small", [0, 2, 5])
+def test_more_new_tokens_than_32_bits_count(torch, gr, R, small):
+    """Requests that ask for 2^30 tokens each: those before the first of them are granted, and no sum wraps round to room."""
+    new = np.full(R, 2 ** 30 - 1, np.int32)
+    new[:small] = 3
+    new[R - 1] = 2
+    stack = np.arange(5000, dtype=np.int32)
+    c = dict(lengths=np.zeros(R, np.int32), new_lengths=new, table=np.full((R, 1024), -1, np.int32), free_blocks=stack, free_count=5000, block=2 ** 20, slots=np.full(40, -7, np.int64))
+    _check(_run(torch, gr, c), c)
+
+
+@pytest.mark.parametrize("R", [3000, 5000])
+def test_many_requests_in_a_graph(torch, gr, R):
+    rng = np.random.default_rng(R)
+    c = _inputs(rng, rng.integers(1, 100, R), [0] * R, 16, 8, 2 * R, 3 * R)
+    c["new_lengths"] = np.clip(c["lengths"] + rng.integers(-20, 4, R), 0, 128).astype(np.int32)
+    to = lambda v: torch.from_numpy(np.ascontiguousarray(v)).cuda()  # noqa: E731
+    start = {k: to(c[k]) for k in ("table", "free_blocks", "slots")}
+    live = {k: v.clone() for k, v in start.items()}
+    old, new, count = to(c["lengths"]), to(c["new_lengths"]), torch.tensor([c["free_count"]], dtype=torch.int32, device="cuda")
+    out = tuple(torch.zeros(n, dtype=torch.int32, device="cuda") for n in (R, 1, R + 1, R))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        gr.gr_page_update(old, new, live["table"], live["free_blocks"], count, 16, live["slots"], out)
+    for _ in range(3):
+        for k, v in start.items():
+            live[k].copy_(v)
+        graph.replay()
+        torch.cuda.synchronize()
+        _check([x.cpu().numpy() for x in (*out, live["slots"], live["table"], live["free_blocks"])], c)
