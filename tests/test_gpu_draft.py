@@ -325,3 +325,25 @@ def test_whole_rows_few_and_many_short_and_long(torch, gr, probs, B, V, n):
                (lambda row, ids, b: row[ids].astype(np.float64)) if probs else (lambda row, ids, b: softmax_mass(row[ids], 1.0)))
     finally:
         gr.gr_destroy(h)
+
+
+@pytest.mark.parametrize("kind,tail_mass", [("float32", 0.0), ("bfloat16", 0.0), ("probs", 0.0), ("probs", 0.2)])
+@pytest.mark.parametrize("V", [900, 20011, 100003])
+def test_draws_do_not_depend_on_the_rows_beside(torch, gr, kind, tail_mass, V):
+    """The same rows alone, in a batch that occupies half the chip, the whole of it, and more: other kernels, the same draws."""
+    gen = torch.Generator(device="cuda").manual_seed(V)
+    x = torch.randn((600, V), device="cuda", generator=gen) * 3
+    x = torch.softmax(x, 1) if kind == "probs" else x.to(getattr(torch, kind))
+    u = torch.rand((600, 7), device="cuda", generator=gen)
+    T = torch.rand(600, device="cuda", generator=gen) + 0.5
+    h = gr.gr_create(600, V, tail_mass=tail_mass)
+    try:
+        for k in (1, 40, 256) if tail_mass else (1, 40, 256, 0):
+            draw = (lambda n: gr.gr_draft(h, x[:n], 7, k, u[:n])) if kind == "probs" else (lambda n: gr.gr_draft_logits(h, x[:n], T[:n], 7, k, u[:n]))
+            drafts, status = draw(600)
+            assert int(status.abs().sum()) == ROW_OK
+            for n in (2, 130, 200, 256, 300, 512):
+                some, status = draw(n)
+                assert torch.equal(some, drafts[:n]) and int(status.abs().sum()) == ROW_OK, (k, n)
+    finally:
+        gr.gr_destroy(h)
