@@ -116,18 +116,31 @@ constexpr float kNone = -__builtin_inff();
 // From here on the chunk's entries are unpacked again: one instruction each, where keeping them would cost a register each.
 __device__ __forceinline__ void unpack_again(uint4& r) { asm volatile("" : "+v"(r.x), "+v"(r.y), "+v"(r.z), "+v"(r.w)); }
 
+template <int CTRL>
+__device__ __forceinline__ float dpp_move_f(float v) { return __int_as_float(dpp_move<CTRL>(__float_as_int(v))); }
+// The largest (the sum) of N values that lie in N lanes side by side, again and again over the wave; N a power of two, 16 at most.
+template <int N>
+__device__ __forceinline__ float lanes_max_f(float v) {
+    if (N > 1) v = fmaxf(v, dpp_move_f<kDppXor1>(v));
+    if (N > 2) v = fmaxf(v, dpp_move_f<kDppXor2>(v));
+    if (N > 4) v = fmaxf(v, dpp_move_f<kDppHalfMirror>(v));
+    if (N > 8) v = fmaxf(v, dpp_move_f<kDppMirror>(v));
+    return v;
+}
+template <int N>
+__device__ __forceinline__ float lanes_sum_f(float v) {
+    if (N > 1) v += dpp_move_f<kDppXor1>(v);
+    if (N > 2) v += dpp_move_f<kDppXor2>(v);
+    if (N > 4) v += dpp_move_f<kDppHalfMirror>(v);
+    if (N > 8) v += dpp_move_f<kDppMirror>(v);
+    return v;
+}
 // The largest and the smallest of a wave's values, the same in all lanes (as in gr_internal.h: no LDS round trips, all lanes active).  NaN is passed over.
 __device__ __forceinline__ float wave_max_f(float v) {
-    v = fmaxf(v, __int_as_float(dpp_move<kDppXor1>(__float_as_int(v))));
-    v = fmaxf(v, __int_as_float(dpp_move<kDppXor2>(__float_as_int(v))));
-    v = fmaxf(v, __int_as_float(dpp_move<kDppHalfMirror>(__float_as_int(v))));
-    v = fmaxf(v, __int_as_float(dpp_move<kDppMirror>(__float_as_int(v))));
-    const int b = __float_as_int(v);
+    const int b = __float_as_int(lanes_max_f<16>(v));
     return fmaxf(fmaxf(__int_as_float(__builtin_amdgcn_readlane(b, 0)), __int_as_float(__builtin_amdgcn_readlane(b, 16))),
                  fmaxf(__int_as_float(__builtin_amdgcn_readlane(b, 32)), __int_as_float(__builtin_amdgcn_readlane(b, 48))));
 }
-template <int CTRL>
-__device__ __forceinline__ float dpp_move_f(float v) { return __int_as_float(dpp_move<CTRL>(__float_as_int(v))); }
 __device__ __forceinline__ float wave_min_f(float v) { return -wave_max_f(-v); }
 
 __device__ __forceinline__ double wave_scan_d(double v) {  // inclusive, all lanes active
@@ -312,16 +325,11 @@ __device__ __forceinline__ float bin_edge(float lo, float hi, int from) {
     return edge > lo ? edge : lo;                         // NaN, too: lo
 }
 
-// The smallest and the largest of what the waves left in `edge`: with many waves a lane to a wave.
+// The smallest and the largest of what the waves left in `edge`.
 template <int NW>
 __device__ __forceinline__ void join_edges(const float* edge, float& lo, float& hi) {
-    if (NW <= 4) {
-#pragma unroll
-        for (int w = 0; w < NW; ++w) { lo = fminf(lo, edge[w]); hi = fmaxf(hi, edge[NW + w]); }
-    } else {
-        const int at = threadIdx.x & (NW - 1);
-        lo = wave_min_f(edge[at]); hi = wave_max_f(edge[NW + at]);
-    }
+    const int at = threadIdx.x & (NW - 1);
+    lo = -lanes_max_f<NW>(-edge[at]); hi = lanes_max_f<NW>(edge[NW + at]);
 }
 
 // Of c > k keys in LDS the largest ones, moved to its begin: at least k, at most `limit`; all threads call it.  Returns how many;

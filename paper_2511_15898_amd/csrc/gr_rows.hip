@@ -88,8 +88,8 @@ __device__ __forceinline__ float find_threshold(const float* tops, int threads, 
     if (lane == 0) { edge[wave] = lo; edge[kNW + wave] = hi; edge[2 * kNW + wave] = lanes; }
     __syncthreads();
     join_edges<kNW>(edge, lo, hi);
-    lanes = wave_sum_f32(lane < kNW ? edge[2 * kNW + lane] : 0.f);
-    if (lanes < static_cast<float>(size * k)) return kNone;                      // the same for all threads
+    lanes = lanes_sum_f<kNW>(edge[2 * kNW + (lane & (kNW - 1))]);
+    if (__any(lanes < static_cast<float>(size * k))) return kNone;               // the same for all threads
     const float per = 255.f / (hi - lo);
 #pragma unroll
     for (int l = 0; l < kLoads; ++l) if (top[l] >= lo) atomicAdd(&hist[static_cast<int>(fminf(fmaxf((top[l] - lo) * per, 0.f), 255.f))], 1);
