@@ -14,7 +14,7 @@ struct DraftLds {
     unsigned long long keys[CAP];
     unsigned long long best[kMaxSupport];                 // by decreasing key
     double mass[kMaxSupport + 64], sum[kMaxSupport + 64 + 1];
-    int ids[kMaxSupport], hist[256], pick[4], count;
+    int ids[kMaxSupport], place[kMaxSupport], hist[256], pick[4], count;       // by id: token, place in `best`
     float edge[2 * (NT / 64)];
 };
 
@@ -76,17 +76,16 @@ __device__ __forceinline__ void draw_from(DraftLds<CAP, NT>& L, int c, int k, do
         kk = __builtin_amdgcn_readfirstlane(L.count);
         __syncthreads();
     }
+    // a thread to a mass: with the order by id, which all waves work on, every wave would work out all exponentials (0.4 us)
+    if (tid < kk) {
+        const unsigned long long key = L.best[tid];
+        L.mass[tid] = PROBS ? static_cast<double>(key_q(key)) : exp((static_cast<double>(key_logit(key)) - static_cast<double>(key_logit(L.best[0]))) * inv_temp);
+    }
     with_registers<kSupportRegs>(kk, [&](auto regs) {
         constexpr int R = decltype(regs)::value;
         int id[R];
-        double mass[R];
-        const float top = key_logit(L.best[0]);
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const unsigned long long key = L.best[min(r * 64 + lane, kk - 1)];
-            id[r] = r * 64 + lane < kk ? key_id(key) : 0x7FFFFFFF;
-            mass[r] = PROBS ? static_cast<double>(key_q(key)) : exp((static_cast<double>(key_logit(key)) - static_cast<double>(top)) * inv_temp);
-        }
+        for (int r = 0; r < R; ++r) id[r] = r * 64 + lane < kk ? key_id(L.best[r * 64 + lane]) : 0x7FFFFFFF;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             int rank = kMaxSupport;
@@ -98,7 +97,7 @@ __device__ __forceinline__ void draw_from(DraftLds<CAP, NT>& L, int c, int k, do
                 for (int o = 0; o < R; ++o) before += __popcll(__ballot(id[o] < mine));
                 rank = lane == at ? before : rank;
             }
-            if (rank < kMaxSupport && r * 64 + lane < kk) { L.ids[rank] = id[r]; L.mass[rank] = mass[r]; }
+            if (rank < kMaxSupport && r * 64 + lane < kk) { L.ids[rank] = id[r]; L.place[rank] = r * 64 + lane; }
         }
     });
     __syncthreads();
@@ -108,7 +107,7 @@ __device__ __forceinline__ void draw_from(DraftLds<CAP, NT>& L, int c, int k, do
     unsigned any = 0u;
 #pragma unroll
     for (int r = 0; r < kSupportRegs; ++r) {
-        const double m = r < per && first + r < kk ? L.mass[first + r] : 0.0;
+        const double m = r < per && first + r < kk ? L.mass[L.place[first + r]] : 0.0;
         own += m;
         cdf[r] = own;
         any |= m > 0.0 ? 1u << r : 0u;
