@@ -29,8 +29,8 @@ __device__ __forceinline__ int owner_of(const int* sums, int n, int x) {
 // count go to arrays of their own, because other workgroups may still be reading the old ones.
 // LDS, by request: exclusive sums of new tokens, new blocks and released blocks; the old length of one that grows, the new one of one that shrinks; OPEN: the block
 // that a growing one has not filled, asked for while the sums are formed (of more requests than kOpenRequests LDS has no room for it; then it is read where it is needed).
-// Bound: the launch and a chain of two reads, scan, search and stores; with many prompt tokens the stores of the slots.  64 requests, a token each 6.0 us; 4096 requests after a
-// verification 15.2 us; a million slots of 512 prompts 10.5 us (0.8 TB/s).
+// Bound: the launch and a chain of two reads, scan, search and stores; with many prompt tokens the stores of the slots.  64 requests, a token each 4.4 us; 4096 requests after a
+// verification 13.1 us; a million slots of 512 prompts 8.7 us (1.0 TB/s).
 constexpr int kOpenRequests = 4096, kPerThread = GR_MAX_REQUESTS / kPageThreads;
 template <bool OPEN>
 __global__ __launch_bounds__(kPageThreads) void pages_kernel(const PageParams pp, const BlockSize bs) {

@@ -360,8 +360,9 @@ __global__ __launch_bounds__(kThreads, SUM && !PROBS ? 4 : 5) void rows_kernel(c
 }
 
 // The drafts of rows that one workgroup each reads: grid = (rows), NT threads.  No slices to join, so one launch does, and the candidates never leave LDS.
-// Bound: for one row a chain of dependent steps, 9.8 us for 32000 float32 logits, k = 64, of them 1.7 until the first tile has come, 1.9 for its threshold, 1.1 for the second tile, 1.7
-// to take the list apart, 1.4 to put 129 candidates in order, 0.8 to put 64 in order by id, 0.6 for the draws.  For 256 rows of 128256 in bfloat16 23 us, of which the read takes 10.
+// Bound: for one row a chain of dependent steps, 9.5 us for 32000 float32 logits, k = 64, of them 1.5 until the first tile has come, 2.2 for its threshold, 1.0 for the second tile, 1.6
+// to take the list apart, 0.8 to put 118 candidates in order, 0.6 to put 64 in order by id, 0.4 for the draws.  For 256 rows of 128256 in bfloat16 22.5 us, of which the read takes 10.
+// What all waves repeat costs four times its instructions on a SIMD with four of them, so it is kept short.
 template <typename T, bool PROBS, int NT>
 __global__ __launch_bounds__(NT) void draft_rows_kernel(const Rows<T> in, int k, double tail_mass, const DraftOut out) {
     __shared__ union { ScanLds<false, NT> scan; DraftLds<kRowCap<NT>, NT> draft; } L;       // the keys are the first of both
