@@ -252,6 +252,7 @@ int gr_draft_logits(gr_handle h, const void* draft_logits, int dtype, long long 
  * token v after beam b is scores[s, b] + log softmax(logits[s, b] / temperature[s])[v], computed in float64 (good to 1.2e-10) and rounded once; ties
  * before that rounding go to the lower beam, within a beam to the larger logit and then the lower token id.  Equal beams tie where their rows begin
  * at the same place modulo 16 bytes; elsewhere their scores may differ by 2.4e-10, though they seldom do, and either may then come first.
+ * (A score beyond float32 is written as -inf; its parent and token are there all the same.)
  * logits      [S, K, V] of `dtype`, row_stride >= V elements from a beam to the next (of the next sequence, too), at any alignment.  -inf: masked.
  * temperature [S] float32, or NULL for 1.
  * scores      [S, K] float32: the beams' sums of log probabilities; -inf: the beam is not in use (its row is not read).

@@ -25,8 +25,9 @@ struct MergeLds {
     int count, bad;
 };
 
-// The candidates in LDS cut to the best M, in order: by score, then the lower beam, then the larger logit, then the lower id.  A wave holds the scores of all in its lanes and takes an eighth of them in turn: its rank is the number of set bits of the comparison of
-// all with it; where scores are equal, which 16-bit logits often are, the rest is compared the same way (one by one it took 44 us for 24 of 12 beams of 1139 in bfloat16).
+// The candidates in LDS cut to the best M, in order: by score, then the lower beam, then the larger logit, then the lower id.  A wave holds the scores of all in its lanes and
+// takes an eighth of them in turn: its rank is the number of set bits of the comparison of all with it; where scores are equal, which 16-bit logits often are, the rest is
+// compared the same way (one by one it took 44 us for 24 of 12 beams of 1139 in bfloat16).
 __device__ __forceinline__ void keep_best(MergeLds& L, int c, int M) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     c = __builtin_amdgcn_readfirstlane(c);                // the same in all lanes, and known to be

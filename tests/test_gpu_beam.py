@@ -1,10 +1,12 @@
 """Beam selection and the states behind it, on the GPU, against plain forms in 64 bits.
 
 Scores are float64 values rounded once to float32: half a step, 2^-24 of the value, beside 1e-9 for the sum of 131072 exponentials (1.04e-10 of the sum at most, the
-bound of the polynomial, and a few 1e-16 per addition).  Where parent and token are others than the plain form's at that rank, theirs must be as good: the plain score of the one chosen lies within 2.4e-10 of
-the score wanted there.  (Let every score be off by e = 1.2e-10 at most, 1.04e-10 of the polynomial, 0.15e-10 of the rounding to 2^-35 and what the additions lose.  The r best by the kernel's scores and the r best by the plain ones have r-th scores that
-differ by e at most, and the plain score of what the kernel chose differs by e from its own.)  So do equal beams, whose rows begin at different places modulo 16 bytes,
-come in either order; where they begin at the same place, the order is the plain form's."""
+bound of the polynomial, and a few 1e-16 per addition).  Where parent and token are others than the plain form's at that rank, theirs must be as good: the plain
+score of the one chosen lies within 2.4e-10 of the score wanted there.  (Let every score be off by e = 1.2e-10 at most: 1.04e-10 of the polynomial, 0.15e-10 of the
+rounding to 2^-35 and what the additions lose.  The r best by the kernel's scores and the r best by the plain ones have r-th scores that differ by e at most, and the
+plain score of what the kernel chose differs by e from its own.)  So do equal beams, whose rows begin at different places modulo 16 bytes, come in either order;
+where they begin at the same place, the order is the plain form's.
+"""
 import numpy as np
 import pytest
 
@@ -390,3 +392,12 @@ def test_few_levels_in_short_rows(torch, gr, S, K, V, M, levels):
     for dtype in (torch.float32, torch.bfloat16):
         y = x.to(dtype)
         _check(_select(torch, gr, y, scores, M), y.float().cpu().numpy(), scores, M, exact=V * y.element_size() % 16 == 0)
+
+
+def test_scores_beyond_float32(torch, gr):
+    """The lowest value at a temperature below 1: the score is one of float64 and -inf in float32, the choice is there."""
+    x = torch.full((1, 2, 700), float(torch.finfo(torch.bfloat16).min), dtype=torch.bfloat16, device="cuda")
+    x[0, 0, 9] = x[0, 1, 4] = 0.0
+    best, parent, token, over, status = _select(torch, gr, x, np.array([[-1.0, -2.0]], np.float32), 5, T=np.array([0.25], np.float32), eos=4)
+    assert best.tolist() == [[-1.0, -2.0] + [-np.inf] * 3] and parent.tolist() == [[0, 1, 0, 0, 0]] and token.tolist() == [[9, 4, 0, 1, 2]] and over.tolist() == [[0, 1, 0, 0, 0]]
+    assert status.tolist() == [0]
