@@ -500,7 +500,8 @@ void launch_draft_rows_as(const RowSource& src, int k, double tail_mass, const D
         constexpr int NT = decltype(threads)::value;
         hipLaunchKernelGGL((draft_rows_kernel<T, PROBS, NT>), dim3(src.rows), dim3(NT), 0, stream, Rows<T>(src), k, tail_mass, out);
     };
-    if (src.rows <= kComputeUnits) run(std::integral_constant<int, 1024>{});
+    const bool one_tile = src.V <= 512 * kLoads * chunk_elements(src.dtype);
+    if (src.rows <= kComputeUnits && !one_tile) run(std::integral_constant<int, 1024>{});
     else if (src.rows <= 2 * kComputeUnits) run(std::integral_constant<int, 512>{});
     else run(std::integral_constant<int, 256>{});
 }
@@ -543,6 +544,8 @@ RowSlices choose_row_slices(int rows, int V, int dtype, int k, bool sums) {
 // 128 of them 18.5, 16.5, 256 of them 24.0, 21.5; of 151936 in float32 one 15.3, 21.3, 128 24.6, 25.6, 256 35.7, 34.0.
 // As many threads as let all rows be read at the same time, 1024 to a compute unit, or, past 512 rows, 256, of which five workgroups fit: 1024 rows of 32000 in bfloat16 take 29.5
 // in slices, 43.1 with 1024 threads, 27.0 with 512, 21.8 with 256; 320 rows 17.3, 20.4, 13.5, 14.8.
+// Rows that 512 threads read in one tile are left to 512, whose barriers and repeated steps cost less: one row of 8192 in float32 takes 6.3 us with 512 and 7.8 with 1024 (kernel), of 16384
+// 8.3 and 7.4; 256 rows of 8192 8.0 and 9.2.
 bool draft_in_one(int rows, int V, int dtype) {
     return rows >= kComputeUnits / 2 || static_cast<long long>(V) <= 3ll * 1024 * kLoads * chunk_elements(dtype);
 }
