@@ -241,7 +241,7 @@ int gr_draft(gr_handle h, const float* q, long long row_stride, int n, int k, co
 
 /*
  * gr_draft for rows given as logits: q = softmax(draft_logits / temperature), in float64 from logits of `dtype` (GR_F32, GR_BF16, GR_F16), never written to
- * memory.  -inf marks a masked token.  temperature [B] float32, positive and finite.  GR_ROW_BAD: a NaN or +inf entry (or finite ones beyond 1e37), a bad
+ * memory; borders between draws lie within 1e-13 of the total of where they belong.  -inf marks a masked token.  temperature [B] float32, positive and finite.  GR_ROW_BAD: a NaN or +inf entry (or finite ones beyond 1e37), a bad
  * temperature, a row without an unmasked token.  A handle with tail_mass > 0 gives GR_EUNSUPPORTED, as in gr_solve_logits.
  */
 int gr_draft_logits(gr_handle h, const void* draft_logits, int dtype, long long row_stride, const float* temperature, int n, int k,

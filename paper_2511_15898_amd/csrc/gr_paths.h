@@ -191,6 +191,7 @@ struct RowChunks {
 // way; sums of many terms are nearer.  The whole part is read off the low bits of y + 1.5 * 2^52; its multiple of 256 goes into the exponent by one addition, since
 // the table's upper words have j 2^12 taken off.  Ten instructions behind the float64 argument and one read of the table.  (A table of 32 entries without bank conflicts
 // and degree 3: 15.)  In two steps, so that several reads are on their way before the first is used.
+// FINE: degree 3, 1.8e-14 either way with its last rounding, one operation more: for draws, whose borders are held to 1e-12 of the total.
 constexpr int kExpEntries = 256;
 constexpr double kExpMagic = 6755399441055744.0;         // 1.5 * 2^52
 struct ExpPart { double rest, entry; int whole; };
@@ -211,9 +212,17 @@ __device__ __forceinline__ ExpPart exp2_256_begin(double x, double scale, double
     e.rest = fma(x, scale, shift_magic - m);
     return e;
 }
+template <bool FINE = false>
 __device__ __forceinline__ double exp2_256_end(const ExpPart& e, double sum) {
-    double p = fma(e.rest, 3.6655651770288774e-06, 2.7076067943688897e-03);
-    p = fma(p, e.rest, 1.0000000000001048);
+    double p;
+    if (FINE) {
+        p = fma(e.rest, 3.308302377575631e-09, 3.66556615675881e-06);
+        p = fma(p, e.rest, 2.7076061740623904e-03);
+        p = fma(p, e.rest, 0.9999999999999825);
+    } else {
+        p = fma(e.rest, 3.6655651770288774e-06, 2.7076067943688897e-03);
+        p = fma(p, e.rest, 1.0000000000001048);
+    }
     return fma(p, __hiloint2double(__double2hiint(e.entry) + (e.whole << 12), __double2loint(e.entry)), sum);
 }
 constexpr double kPerTemp = 369.32993046757463;           // 256 / ln 2
@@ -225,6 +234,7 @@ __device__ __forceinline__ void fill_exp_table(double* tab) {        // by 256 t
 
 // A wave's sum of exponentials: of exp((x - ref) / T), but for a factor near 1, ref the largest entry of its first tile that has any.  A later entry may lie above ref
 // (float64 has room for e^433 of them) until that is used up; then the sum is brought to a new reference.
+template <bool FINE = false>
 struct ExpSum {
     double sum = 0.0, scale, shift = 0.0;                 // of 2^(place(x) / 256); scale: kPerTemp / T; shift: -ref * scale, rounded to a whole number
     float ref = kNone, floor = kNone, ceiling = kNone;    // floor: entries below it count as if they were e^-474 of the reference; above the ceiling there is no room
@@ -246,7 +256,7 @@ struct ExpSum {
     // the sum as one of exp((x - to) / T), `to` not below ref
     __device__ __forceinline__ double rebased(float to, const double* tab) const {
         const double y = fmax(-place(static_cast<double>(to)), static_cast<double>(kLowest));
-        return ref > kNone ? sum * exp2_256_end(exp2_256_begin(y, tab), 0.0) : 0.0;
+        return ref > kNone ? sum * exp2_256_end<FINE>(exp2_256_begin(y, tab), 0.0) : 0.0;
     }
     // from here on entries up to `most` (this lane's) come
     __device__ __forceinline__ void raise(float most, const double* tab) {
@@ -254,7 +264,7 @@ struct ExpSum {
             most = wave_max_f(most);
             sum = rebased(most, tab);
             refer(most);
-            sum *= exp2_256_end(exp2_256_begin(place(static_cast<double>(ref)), tab), 0.0);
+            sum *= exp2_256_end<FINE>(exp2_256_begin(place(static_cast<double>(ref)), tab), 0.0);
         }
     }
     // kEight entries per lane.  A NaN makes the sum NaN.
@@ -272,7 +282,7 @@ struct ExpSum {
                 for (int i = 0; i < 4; ++i) e[i] = exp2_256_begin(static_cast<double>(x[i0 + i]), scale, shift_magic, tab);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum = exp2_256_end(e[i], sum);
+                for (int i = 0; i < 4; ++i) sum = exp2_256_end<FINE>(e[i], sum);
                 __builtin_amdgcn_sched_barrier(0);
             }
         } else {
@@ -282,7 +292,7 @@ struct ExpSum {
                 float v = x[0];
 #pragma unroll
                 for (int j = 1; j < kEight; ++j) v = i == j ? x[j] : v;
-                const double upto = exp2_256_end(exp2_256_begin(fmax(place(static_cast<double>(v)), static_cast<double>(kLowest)), tab), sum);
+                const double upto = exp2_256_end<FINE>(exp2_256_begin(fmax(place(static_cast<double>(v)), static_cast<double>(kLowest)), tab), sum);
                 sum = v == v ? upto : static_cast<double>(v);
             }
         }

@@ -128,7 +128,7 @@ struct ScanLds {
     double red[NT / 64], tab[EXP ? kExpEntries : 1];
 };
 // What a thread has of a slice behind a scan: how many keys lie in LDS (the same for all), whether it met a bad entry, its part of the sum (with its wave's reference).
-struct Scanned { int found, bad; double total; ExpSum es; };
+struct Scanned { int found, bad; double total; ExpSum<> es; };
 
 template <typename T, bool PROBS, bool EXP, int NT>
 __device__ __forceinline__ Scanned scan_slice(ScanLds<EXP, NT>& L, const Rows<T>& in, int row, const RowChunks<T>& x, int c_first, int c_end, int k) {
@@ -167,7 +167,7 @@ __device__ __forceinline__ Scanned scan_slice(ScanLds<EXP, NT>& L, const Rows<T>
     float theta = kNone;                                  // entries below it are no candidates
     bool over = false;                                    // more candidates than LDS holds
     double total = 0.0;
-    ExpSum es(scale);
+    ExpSum<> es(scale);
     const float least = PROBS ? 0.f : kNone;              // entries must lie above it
     const auto key_of = [](float v, int id) { return PROBS ? make_key(v, id) : make_key_logit(v, id); };
     // the list taken apart: its entries that reach the threshold become keys
@@ -259,11 +259,11 @@ __device__ __forceinline__ Scanned scan_slice(ScanLds<EXP, NT>& L, const Rows<T>
                     for (int j = 0; j < N; ++j) { const float v = Packed<T>::get(now[l], j); bad |= static_cast<int>(l < loads) & static_cast<int>(v != v); }
             } else
 #pragma unroll
-                for (int l = 0; l < kLoads; l += ExpSum::kEight / N) {
+                for (int l = 0; l < kLoads; l += ExpSum<>::kEight / N) {
                     if (l >= loads) continue;
-                    float v[ExpSum::kEight];
+                    float v[ExpSum<>::kEight];
 #pragma unroll
-                    for (int j = 0; j < ExpSum::kEight; ++j) v[j] = l + j / N < loads ? Packed<T>::get(now[l + j / N], j % N) : kNone;
+                    for (int j = 0; j < ExpSum<>::kEight; ++j) v[j] = l + j / N < loads ? Packed<T>::get(now[l + j / N], j % N) : kNone;
                     es.add(v, tab);
                 }
         }
@@ -430,13 +430,13 @@ __device__ __forceinline__ PieceMass piece_mass(const RowChunks<T>& x, int piece
         bad |= static_cast<int>(top > 3.0e38f);
         ref = wave_max_f(top);
         if (ref > kNone && scale > 0.0) {
-            ExpSum es(scale);
+            ExpSum<true> es(scale);                       // the draws' borders stand on these sums
             es.refer(ref);
 #pragma unroll
-            for (int l = 0; l < kLoads; l += ExpSum::kEight / N) {
-                float v[ExpSum::kEight];
+            for (int l = 0; l < kLoads; l += ExpSum<>::kEight / N) {
+                float v[ExpSum<>::kEight];
 #pragma unroll
-                for (int j = 0; j < ExpSum::kEight; ++j) v[j] = Packed<T>::get(r[l + j / N], j % N);
+                for (int j = 0; j < ExpSum<>::kEight; ++j) v[j] = Packed<T>::get(r[l + j / N], j % N);
                 es.add(v, tab);
             }
             sum = es.rebased(ref, tab);                   // NaN if an entry is

@@ -1,0 +1,75 @@
+"""Rows, temperatures and scores at the ends of what the calls accept, drafts and beam selections against the plain forms in 64 bits.  Scores and the order of beams are held to what
+test_gpu_beam.py derives for them, draws to the border of test_gpu_draft.py: sums of float64 exponentials whose relative error is 1.8e-14 at most (the rounding of a
+polynomial's last step included), so borders lie within 4e-14 of the total of where they belong, and 1e-12 leaves room."""
+import numpy as np
+import pytest
+
+from beside_forms import ROW_BAD, ROW_OK, beam_select, draft_support, draw, softmax_mass
+from test_gpu_beam import _check as check_beams, _select as select
+
+pytestmark = pytest.mark.gpu
+BORDER = 1e-12
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    return torch
+
+
+@pytest.fixture(scope="module")
+def gr():
+    from paper_2511_15898_amd import binding
+    return binding
+
+
+def _drafts(torch, gr, x, k, uniforms, T=None):
+    """Drafts of x [B, V] on the GPU (probabilities if T is None), as arrays; the call made twice."""
+    B, V = x.shape
+    n = uniforms.shape[1]
+    h = gr.gr_create(B, V, max_n=n)
+    u = torch.from_numpy(uniforms).cuda()
+    try:
+        call = (lambda: gr.gr_draft(h, x, n, k, u)) if T is None else (lambda: gr.gr_draft_logits(h, x, torch.from_numpy(T).cuda(), n, k, u))
+        drafts, status = call()
+        again, _ = call()
+        assert torch.equal(drafts, again)
+        return drafts.cpu().numpy(), status.cpu().numpy()
+    finally:
+        gr.gr_destroy(h)
+
+
+def _check_drafts(drafts, rows, k, uniforms, T=None, some=None):
+    for b in range(len(rows)) if some is None else some:
+        ids = draft_support(rows[b], k)
+        mass = rows[b, ids].astype(np.float64) if T is None else softmax_mass(rows[b, ids], float(T[b]))
+        for j, (token, near) in enumerate(draw(mass, ids, uniforms[b])):
+            assert drafts[b, j] == token or near < BORDER, (b, j, int(drafts[b, j]), token, near)
+
+
+def _uniforms(seed, B, n):
+    return np.minimum(np.random.default_rng(seed).random((B, n)).astype(np.float32), np.float32(1.0 - 2.0 ** -24))
+
+
+@pytest.mark.parametrize("V, many", [(900, 1), (5003, 1), (5003, 8), (40001, 1)])
+def test_draws_from_whole_rows_next_to_a_border(torch, gr, V, many):
+    """Uniforms that lie between 1.5 and 30 millionths of a millionth of the total from a border of the distribution, which float64 masses tell apart, in rows of heavy tails."""
+    rng = np.random.default_rng(V)
+    rows, uniforms = [], []
+    while len(rows) < 40:
+        x = (4.0 * rng.gumbel(size=V)).astype(np.float32)
+        cdf = np.cumsum(softmax_mass(x, 1.0).astype(np.longdouble))
+        cdf = cdf[:-1] / cdf[-1]
+        u = cdf.astype(np.float32)
+        far = np.abs(u.astype(np.longdouble) - cdf)
+        others = np.minimum(np.diff(cdf, prepend=np.longdouble(-1)), np.diff(cdf, append=np.longdouble(2)))
+        near = np.flatnonzero((cdf > 0.05) & (far > 1.5e-12) & (far < 3e-11) & (u < 1) & (others > 1e-10))
+        if len(near):
+            rows.append(x)
+            uniforms.append([u[near[i % len(near)]] for i in range(6)])
+    rows, u = np.tile(np.stack(rows), (many, 1)), np.tile(np.array(uniforms, np.float32), (many, 1))
+    T = np.ones(len(rows), np.float32)
+    drafts, status = _drafts(torch, gr, torch.from_numpy(rows).cuda(), 0, u, T)
+    assert (status == ROW_OK).all()
+    _check_drafts(drafts, rows, 0, u, T, some=range(40))
+    assert many == 1 or (drafts.reshape(many, 40, 6) == drafts[:40]).all()
