@@ -112,6 +112,7 @@ template <> struct Packed<_Float16> {
     static constexpr unsigned kNoneBits = 0xFC00u;
 };
 constexpr float kNone = -__builtin_inff();
+constexpr float kMostFloat = 3.402823466e38f;
 
 // From here on the chunk's entries are unpacked again: one instruction each, where keeping them would cost a register each.
 __device__ __forceinline__ void unpack_again(uint4& r) { asm volatile("" : "+v"(r.x), "+v"(r.y), "+v"(r.z), "+v"(r.w)); }
@@ -250,7 +251,8 @@ struct ExpSum {
         // the same in all lanes, and known to be
         set(__int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(most))));
         plain = __builtin_amdgcn_readfirstlane(plain) != 0;
-        floor = static_cast<float>(static_cast<double>(ref) + static_cast<double>(kLowest) / scale);
+        // not below the lowest float: rounded to -inf, it would let masked entries into the arm for those at or above it
+        floor = fmaxf(static_cast<float>(static_cast<double>(ref) + static_cast<double>(kLowest) / scale), -kMostFloat);
         ceiling = static_cast<float>(static_cast<double>(ref) + static_cast<double>(kHighest) / scale);
     }
     // the sum as one of exp((x - to) / T), `to` not below ref

@@ -73,3 +73,24 @@ def test_draws_from_whole_rows_next_to_a_border(torch, gr, V, many):
     assert (status == ROW_OK).all()
     _check_drafts(drafts, rows, 0, u, T, some=range(40))
     assert many == 1 or (drafts.reshape(many, 40, 6) == drafts[:40]).all()
+
+
+@pytest.mark.parametrize("T", [7.0e35, 1.0e36, 1.0e37, 2.9e38])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("V", [1003, 40001])
+def test_temperatures_next_to_the_largest_float(torch, gr, T, dtype, V):
+    """Nothing lies below the lowest entry that such a temperature sets apart, but masked entries, and the places beside a row that begins at no 16-byte boundary, still count nothing."""
+    S, K, M = 3, 3, 6
+    rng = np.random.default_rng(V)
+    x = np.minimum(0.4e36 * rng.gumbel(size=(S, K, V)), 9e36).astype(np.float32)
+    x[1] = (x[1] * np.float32(1e-36)).astype(np.float32)                     # ordinary logits: as good as equal
+    x[2, :, 3::4] = -np.inf
+    x = torch.from_numpy(x).cuda().to(getattr(torch, dtype))
+    rows, temps = x.float().cpu().numpy(), np.full(S, T, np.float32)
+    scores = rng.uniform(-9.0, -8.0, (S, K)).astype(np.float32)
+    check_beams(select(torch, gr, x, scores, M, temps), rows, scores, M, temps)
+    u, per_row = _uniforms(V, S * K, 9), np.full(S * K, T, np.float32)
+    for k in (0, 100):
+        drafts, status = _drafts(torch, gr, x.view(S * K, V), k, u, per_row)
+        assert (status == ROW_OK).all()
+        _check_drafts(drafts, rows.reshape(S * K, V), k, u, per_row)
