@@ -253,7 +253,10 @@ struct ExpSum {
         plain = __builtin_amdgcn_readfirstlane(plain) != 0;
         // not below the lowest float: rounded to -inf, it would let masked entries into the arm for those at or above it
         floor = fmaxf(static_cast<float>(static_cast<double>(ref) + static_cast<double>(kLowest) / scale), -kMostFloat);
-        ceiling = static_cast<float>(static_cast<double>(ref) + static_cast<double>(kHighest) / scale);
+        // rounded down: the float above it may lie hundreds of temperatures further
+        const double room = static_cast<double>(ref) + static_cast<double>(kHighest) / scale;
+        ceiling = static_cast<float>(room);
+        if (static_cast<double>(ceiling) > room) ceiling = __int_as_float(__float_as_int(ceiling) + (ceiling > 0.f ? -1 : 1));
     }
     // the sum as one of exp((x - to) / T), `to` not below ref
     __device__ __forceinline__ double rebased(float to, const double* tab) const {

@@ -94,3 +94,24 @@ def test_temperatures_next_to_the_largest_float(torch, gr, T, dtype, V):
         drafts, status = _drafts(torch, gr, x.view(S * K, V), k, u, per_row)
         assert (status == ROW_OK).all()
         _check_drafts(drafts, rows.reshape(S * K, V), k, u, per_row)
+
+
+@pytest.mark.parametrize("top, T", [(100.0, 1.0e-8), (20.0, 2.48e-9), (10.0, 1.2e-9), (-3.0, 3.0e-10), (1.0, 1.5e-10), (1.0, 1.4e-10)])
+def test_temperatures_of_a_thousandth_of_the_last_digit(torch, gr, top, T):
+    """The row's largest entry is the float behind the largest one so far, and hundreds of temperatures above it: the sum is brought to it although nothing lies between the two.
+    1024 rows, so that each is one workgroup's and the two lie in the hands of one wave, tiles of 4096 entries apart."""
+    S, K, V, M = 64, 16, 9000, 3
+    x = torch.full((S, K, V), top - 5.0, device="cuda")
+    x[:, :, 5] = top
+    x[:, ::2, 5 + 4096] = float(np.nextafter(np.float32(top), np.float32(np.inf)))
+    x[:, 1::2, 5 + 8192] = float(np.nextafter(np.float32(top), np.float32(np.inf)))
+    scores = np.random.default_rng(0).uniform(-9.0, -1.0, (S, K)).astype(np.float32)
+    temps = np.full(S, T, np.float32)
+    got = select(torch, gr, x, scores, M, temps)
+    some = [0, 17, S - 1]
+    check_beams([v[some] for v in got], x[some].cpu().numpy(), scores[some], M, temps[some])
+    u, per_row = _uniforms(1, S * K, 3), np.full(S * K, T, np.float32)
+    for k in (0, 2):
+        drafts, status = _drafts(torch, gr, x.view(S * K, V), k, u, per_row)
+        assert (status == ROW_OK).all()
+        _check_drafts(drafts, x.view(S * K, V).cpu().numpy(), k, u, per_row, some=[0, 1, S * K - 1])
