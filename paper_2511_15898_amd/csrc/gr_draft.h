@@ -176,7 +176,7 @@ __device__ __forceinline__ void draw_whole(const Rows<T>& in, int row, int draw,
     const bool found = piece >= 0;
     if (!found) piece = last;
     const double rest = found ? target - before : __builtin_inf();
-    const RowChunks<T> x(in.row(row), in.V);
+    const RowChunks<T, PROBS> x(in.row(row), in.V);
     const int c0 = piece * 64 * kLoads;
     const bool whole = x.inside(c0, c0 + 64 * kLoads);
     double done = 0.0;
@@ -191,7 +191,7 @@ __device__ __forceinline__ void draw_whole(const Rows<T>& in, int row, int draw,
         double e[N], mine = 0.0;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            e[j] = v[j] == kNone ? 0.0 : (PROBS ? static_cast<double>(v[j]) : exp((static_cast<double>(v[j]) - top) * inv_temp));
+            e[j] = PROBS ? static_cast<double>(v[j]) : (v[j] == kNone ? 0.0 : exp((static_cast<double>(v[j]) - top) * inv_temp));
             mine += e[j];
             if (e[j] > 0.0) last_id = x.id(c, j);
         }

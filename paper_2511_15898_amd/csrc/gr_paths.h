@@ -156,8 +156,8 @@ __device__ __forceinline__ double wave_scan_d(double v) {  // inclusive, all lan
 
 
 // A row as 16-byte chunks at 16-byte boundaries, wherever it begins: chunk c holds elements [c N - lead, c N - lead + N).  Chunks that reach
-// over an end of the row are read element by element, entries outside it are -inf.
-template <typename T>
+// over an end of the row are read element by element; entries outside it are -inf, of probabilities 0 (a -inf among them is a bad entry of the row's own).
+template <typename T, bool PROBS>
 struct RowChunks {
     static constexpr int N = Packed<T>::N;
     const T* row; int V, lead, chunks;
@@ -176,7 +176,7 @@ struct RowChunks {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             const long long i = static_cast<long long>(c) * N - lead + j;
-            w[j * 4 / N] |= ((i >= 0 && i < V) ? Packed<T>::bits(row[i]) : Packed<T>::kNoneBits) << (j * 32 * 4 / N % 32);
+            w[j * 4 / N] |= ((i >= 0 && i < V) ? Packed<T>::bits(row[i]) : (PROBS ? 0u : Packed<T>::kNoneBits)) << (j * 32 * 4 / N % 32);
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }

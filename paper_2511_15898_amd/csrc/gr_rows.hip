@@ -131,7 +131,7 @@ struct ScanLds {
 struct Scanned { int found, bad; double total; ExpSum<> es; };
 
 template <typename T, bool PROBS, bool EXP, int NT>
-__device__ __forceinline__ Scanned scan_slice(ScanLds<EXP, NT>& L, const Rows<T>& in, int row, const RowChunks<T>& x, int c_first, int c_end, int k) {
+__device__ __forceinline__ Scanned scan_slice(ScanLds<EXP, NT>& L, const Rows<T>& in, int row, const RowChunks<T, PROBS>& x, int c_first, int c_end, int k) {
     constexpr int N = Packed<T>::N, kTileChunks = NT * kLoads, kNW = NT / 64, kCap = kRowCap<NT>;
     constexpr bool kExp = EXP;
     unsigned long long* const keys = L.keys;
@@ -229,7 +229,7 @@ __device__ __forceinline__ Scanned scan_slice(ScanLds<EXP, NT>& L, const Rows<T>
         for (int l = 0; l < kLoads; ++l) now[l] = next[l];
         fetch(c0 + kTileChunks);
         const int loads = min(kLoads, (c_end - c0 + NT - 1) / NT);     // of the last tile maybe fewer
-        // Entries outside the row are -inf.  Bad: NaN, +inf (logits), negative entries (probabilities).
+        // Bad: NaN, +inf (logits), negative entries (probabilities).
         float top[kLoads], most = kNone, probe = 0.f;
 #pragma unroll
         for (int l = 0; l < kLoads; ++l) {
@@ -240,8 +240,8 @@ __device__ __forceinline__ Scanned scan_slice(ScanLds<EXP, NT>& L, const Rows<T>
                 const float v = Packed<T>::get(now[l], j);
                 top[l] = fmaxf(top[l], v);
                 if (PROBS) {
-                    bad |= static_cast<int>(!(v >= 0.f)) & static_cast<int>(v != kNone);
-                    total += static_cast<double>(v == kNone ? 0.f : v);
+                    bad |= static_cast<int>(!(v >= 0.f));
+                    total += static_cast<double>(v);
                 } else if (!kExp) probe += v;
             }
             most = fmaxf(most, top[l]);
@@ -266,6 +266,11 @@ __device__ __forceinline__ Scanned scan_slice(ScanLds<EXP, NT>& L, const Rows<T>
                     for (int j = 0; j < ExpSum<>::kEight; ++j) v[j] = l + j / N < loads ? Packed<T>::get(now[l + j / N], j % N) : kNone;
                     es.add(v, tab);
                 }
+        }
+        if (PROBS && theta == kNone) {
+            // chunks behind the slice, zeros, have no part in the threshold
+#pragma unroll
+            for (int l = 0; l < kLoads; ++l) if (c0 + l * NT + tid >= c_end) top[l] = kNone;
         }
         if (theta == kNone) theta = find_threshold<PROBS, NT>(top, min(NT, c_end - c0), k, hist, edge);
         unsigned long long hit[kLoads];
@@ -326,7 +331,7 @@ __global__ __launch_bounds__(kThreads, SUM && !PROBS ? 4 : 5) void rows_kernel(c
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int row = blockIdx.x / splits, s = blockIdx.x - row * splits;
     if (in.skip(row)) return;
-    const RowChunks<T> x(in.row(row), in.V);
+    const RowChunks<T, PROBS> x(in.row(row), in.V);
     Scanned mine = scan_slice<T, PROBS, kExp, kThreads>(L, in, row, x, s * per, min(x.chunks, s * per + per), k);
     int found = mine.found;
     const int room = min(kSelCap / splits, limit);        // k at least
@@ -371,7 +376,7 @@ __global__ __launch_bounds__(NT) void draft_rows_kernel(const Rows<T> in, int k,
     __shared__ int any_bad;
     const int tid = threadIdx.x, lane = tid & 63, row = blockIdx.x;
     if (tid == 0) any_bad = 0;
-    const RowChunks<T> x(in.row(row), in.V);
+    const RowChunks<T, PROBS> x(in.row(row), in.V);
     const Uniforms<NT> uniforms(out, row);
     const float t = PROBS ? 1.f : in.temperature_of(row);
     const Scanned mine = scan_slice<T, PROBS, false, NT>(L.scan, in, row, x, 0, x.chunks, k);
@@ -399,7 +404,7 @@ __global__ __launch_bounds__(NT) void draft_rows_kernel(const Rows<T> in, int k,
 // largest entry as ref, scale 0 for a bad temperature.  A bad entry makes it NaN, and with it the row's total.
 struct PieceMass { double mass; float ref; };
 template <typename T, bool PROBS>
-__device__ __forceinline__ PieceMass piece_mass(const RowChunks<T>& x, int piece, double scale, const double* tab) {
+__device__ __forceinline__ PieceMass piece_mass(const RowChunks<T, PROBS>& x, int piece, double scale, const double* tab) {
     constexpr int N = Packed<T>::N;
     const int lane = threadIdx.x & 63;
     int bad = static_cast<int>(!(scale > 0.0));
@@ -419,8 +424,8 @@ __device__ __forceinline__ PieceMass piece_mass(const RowChunks<T>& x, int piece
         for (int j = 0; j < N; ++j) {
             const float v = Packed<T>::get(r[l], j);
             if (PROBS) {
-                bad |= static_cast<int>(!(v >= 0.f)) & static_cast<int>(v != kNone);
-                sum += static_cast<double>(v == kNone ? 0.f : v);
+                bad |= static_cast<int>(!(v >= 0.f));
+                sum += static_cast<double>(v);
             } else top = fmaxf(top, v);
         }
         unpack_again(r[l]);
@@ -465,7 +470,7 @@ __global__ __launch_bounds__(kThreads) void masses_kernel(const Rows<T> in, int 
     if (!PROBS) { fill_exp_table(tab); __syncthreads(); }
     const int piece = (blockIdx.x - row * groups) * kWaves + (tid >> 6);
     if (piece >= pieces) return;                          // whole waves
-    const PieceMass m = piece_mass<T, PROBS>(RowChunks<T>(in.row(row), in.V), piece, PROBS ? 1.0 : scale_of(in, row), tab);
+    const PieceMass m = piece_mass<T, PROBS>(RowChunks<T, PROBS>(in.row(row), in.V), piece, PROBS ? 1.0 : scale_of(in, row), tab);
     if ((tid & 63) == 0) {
         const size_t at = static_cast<size_t>(row) * stride + piece;
         mass[at] = m.mass; refs[at] = m.ref;
@@ -480,7 +485,7 @@ __global__ __launch_bounds__(NT) void draft_whole_rows_kernel(const Rows<T> in, 
     __shared__ float refs[kLdsPieces];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = blockIdx.x;
     if (!PROBS) { if (tid < kExpEntries) fill_exp_table(tab); __syncthreads(); }
-    const RowChunks<T> x(in.row(row), in.V);
+    const RowChunks<T, PROBS> x(in.row(row), in.V);
     const double scale = PROBS ? 1.0 : scale_of(in, row);
     for (int piece = wave; piece < pieces; piece += NT / 64) {
         const PieceMass m = piece_mass<T, PROBS>(x, piece, scale, tab);

@@ -115,3 +115,22 @@ def test_temperatures_of_a_thousandth_of_the_last_digit(torch, gr, top, T):
         drafts, status = _drafts(torch, gr, x.view(S * K, V), k, u, per_row)
         assert (status == ROW_OK).all()
         _check_drafts(drafts, x.view(S * K, V).cpu().numpy(), k, u, per_row, some=[0, 1, S * K - 1])
+
+
+@pytest.mark.parametrize("B, V", [(6, 50), (6, 1001), (6, 9001), (6, 70001), (6, 200003), (200, 9001), (600, 1003)])
+@pytest.mark.parametrize("k", [8, 0])
+def test_minus_infinity_is_no_probability(torch, gr, B, V, k):
+    """At either end of a row, where what lies beside it in its 16 bytes is not the row's, and in the middle; the other entries sum to 1, so nothing else is wrong with it."""
+    q = np.random.default_rng(V).random((B, V))
+    at = {0: 0, 1: V - 1, 2: V // 2, 4: 1}
+    for b, i in at.items():
+        q[b, i] = 0.0
+    q = (q / q.sum(1, keepdims=True)).astype(np.float32)
+    for b, i in at.items():
+        q[b, i] = -np.inf
+    u = _uniforms(V, B, 3)
+    drafts, status = _drafts(torch, gr, torch.from_numpy(q).cuda(), k, u)
+    bad = np.zeros(B, bool)
+    bad[list(at)] = True
+    assert (status[bad] == ROW_BAD).all() and (drafts[bad] == -1).all() and (status[~bad] == ROW_OK).all()
+    _check_drafts(drafts, q, k, u, some=[3, 5, B - 1] if B > 6 else [3, 5])
