@@ -434,11 +434,14 @@ __device__ __forceinline__ unsigned long long make_key(float q, int id) {
     return (static_cast<unsigned long long>(__float_as_uint(q)) << 32) |
            static_cast<unsigned long long>(0xFFFFFFFFu - static_cast<unsigned>(id));
 }
-// The same for a draft logit (any finite float): its bit pattern made monotone over the whole line.
+// A float's bit pattern made monotone over the whole line; -0.0 is 0.0 (the sum of both), so that zeros tie whatever their signs.
+__device__ __forceinline__ unsigned mono32(float x) {
+    const unsigned b = __float_as_uint(x + 0.f);
+    return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
+}
+// The same for a draft logit (any finite float).
 __device__ __forceinline__ unsigned long long make_key_logit(float d, int id) {
-    const unsigned b = __float_as_uint(d);
-    const unsigned mono = (b & 0x80000000u) ? ~b : (b | 0x80000000u);
-    return (static_cast<unsigned long long>(mono) << 32) | static_cast<unsigned long long>(0xFFFFFFFFu - static_cast<unsigned>(id));
+    return (static_cast<unsigned long long>(mono32(d)) << 32) | static_cast<unsigned long long>(0xFFFFFFFFu - static_cast<unsigned>(id));
 }
 // A double as a 64-bit pattern that rises with it (any finite value or infinity).
 __device__ __forceinline__ unsigned long long mono64(double x) {
@@ -447,10 +450,6 @@ __device__ __forceinline__ unsigned long long mono64(double x) {
 }
 __device__ __forceinline__ double unmono64(unsigned long long m) {
     return __longlong_as_double(static_cast<long long>((m >> 63) ? m & 0x7FFFFFFFFFFFFFFFull : ~m));
-}
-__device__ __forceinline__ unsigned mono32(float x) {
-    const unsigned b = __float_as_uint(x);
-    return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
 // The value whose decreasing order is that of q/p for rows given as logits: q/p is proportional to
 // exp(d / Td - t / Tt).  With one temperature that is the order of d - t, exact in float64 for float32 logits; with

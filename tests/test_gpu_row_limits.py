@@ -134,3 +134,42 @@ def test_minus_infinity_is_no_probability(torch, gr, B, V, k):
     bad[list(at)] = True
     assert (status[bad] == ROW_BAD).all() and (drafts[bad] == -1).all() and (status[~bad] == ROW_OK).all()
     _check_drafts(drafts, q, k, u, some=[3, 5, B - 1] if B > 6 else [3, 5])
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("V, k", [(2, 1), (300, 7), (5001, 40), (20011, 256), (100003, 3)])
+def test_zeros_of_either_sign_are_equal_logits(torch, gr, dtype, V, k):
+    """What a product with a mask leaves: the lower token comes first, whatever the signs, among the drafts' k largest as among the continuations."""
+    B = 4
+    rng = np.random.default_rng(V)
+    x = np.where(rng.random((B, V)) < 0.5, np.float32(-0.0), np.float32(0.0))
+    x[0, 0], x[0, 1] = -0.0, 0.0
+    x[1, 5::6] = -2.0
+    x[2, 3::50] = 1.0
+    t = torch.from_numpy(x).cuda().to(getattr(torch, dtype))
+    u, T = _uniforms(V, B, 8), np.ones(B, np.float32)
+    drafts, status = _drafts(torch, gr, t, k, u, T)
+    assert (status == ROW_OK).all()
+    _check_drafts(drafts, x, k, u, T)
+    M, scores = min(k, 64), np.array([[-1.0, -1.5, -1.25, -1.0]], np.float32)
+    check_beams(select(torch, gr, t[None], scores, M), x[None], scores, M, exact=V * t.element_size() % 16 == 0)
+
+
+@pytest.mark.parametrize("V, k", [(300, 7), (5001, 256), (5001, 300), (20011, 1000)])
+def test_the_solver_takes_the_same_tokens_of_equal_zeros(torch, gr, V, k):
+    """gr_solve_logits: the k largest draft logits, ties to the lower token, so that the drafts lie in its support."""
+    B = 3
+    rng = np.random.default_rng(V + k)
+    d = np.where(rng.random((B, V)) < 0.5, np.float32(-0.0), np.float32(0.0))
+    d[1, rng.permutation(V)[:k // 2]] = 1.0
+    target = rng.standard_normal((B, V)).astype(np.float32)
+    to = lambda v: torch.from_numpy(v).cuda()  # noqa: E731
+    h = gr.gr_create(B, V, max_k=k, max_n=1)
+    try:
+        acc, status = gr.gr_solve_logits(h, to(target), to(d), torch.ones(B, device="cuda"), 1, k, 1e-4)
+        assert bool((status <= 1).all())                                    # equal logits: the truncation may take more variables than there is room for
+        for b in range(B):
+            taken = gr.gr_policy_export_row(h, b, k, "cuda")["order"].cpu().numpy()
+            assert np.array_equal(np.sort(taken), draft_support(d[b], k)), b
+    finally:
+        gr.gr_destroy(h)
