@@ -192,7 +192,8 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(const Rows<fl
     from = owner ? __builtin_amdgcn_readlane(from, __ffsll(owner) - 1) : 0;      // fewer threads than M have met any: all that reach theta
     const auto append = [&](double value, unsigned long long key, int b) {
         const int slot = atomicAdd(&L.count, 1);
-        if (slot < kMergeCap) { L.value[slot] = mono64(value); L.key[slot] = key; L.beam[slot] = b; }
+        // plus 0.0: a score rounded to -0.0, or given as one, ties with 0.0
+        if (slot < kMergeCap) { L.value[slot] = mono64(value + 0.0); L.key[slot] = key; L.beam[slot] = b; }
     };
     // a finished beam's one candidate
     const auto append_finished = [&]() {

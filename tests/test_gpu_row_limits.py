@@ -173,3 +173,16 @@ def test_the_solver_takes_the_same_tokens_of_equal_zeros(torch, gr, V, k):
             assert np.array_equal(np.sort(taken), draft_support(d[b], k)), b
     finally:
         gr.gr_destroy(h)
+
+
+def test_scores_of_zero_tie_whatever_their_sign(torch, gr):
+    """Certain continuations, ended beams at 0 and at -0.0: equal scores, so the lower beam comes first."""
+    V, M, eos = 40, 5, 7
+    x = torch.full((4, 3, V), -float("inf"), device="cuda")
+    x[:, :, 9] = 3.0                                                        # the one token, of probability 1
+    scores = np.zeros((4, 3), np.float32)
+    scores[2, 1] = scores[3, 0] = -0.0
+    finished = np.array([[0, 1, 0], [1, 0, 1], [0, 1, 1], [1, 1, 0]], np.uint8)
+    best, parent, token, over, status = select(torch, gr, x, scores, M, finished=finished, eos=eos)
+    assert status.tolist() == [0] * 4 and (parent == [[0, 1, 2, -1, -1]] * 4).all() and (best[:, :3] == 0).all()
+    assert (token[:, :3] == np.where(finished, eos, 9)).all() and (over[:, :3] == finished).all()
