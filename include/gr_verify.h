@@ -241,7 +241,7 @@ int gr_draft(gr_handle h, const float* q, long long row_stride, int n, int k, co
 
 /*
  * gr_draft for rows given as logits: q = softmax(draft_logits / temperature), in float64 from logits of `dtype` (GR_F32, GR_BF16, GR_F16), never written to
- * memory; borders between draws lie within 1e-13 of the total of where they belong.  -inf marks a masked token.  temperature [B] float32, positive and finite.  GR_ROW_BAD: a NaN or +inf entry (or finite ones beyond 1e37), a bad
+ * memory; borders between draws lie within 1e-13 of the total of where they belong.  -inf marks a masked token.  temperature [B] float32, positive and finite.  GR_ROW_BAD: a NaN, an entry above 1e37, a bad
  * temperature, a row without an unmasked token.  A handle with tail_mass > 0 gives GR_EUNSUPPORTED, as in gr_solve_logits.
  */
 int gr_draft_logits(gr_handle h, const void* draft_logits, int dtype, long long row_stride, const float* temperature, int n, int k,
@@ -261,7 +261,7 @@ int gr_draft_logits(gr_handle h, const void* draft_logits, int dtype, long long 
  * S K rows within the handle's max_B, V within its max_V, 1 <= K, M <= GR_MAX_BEAMS.
  * out_scores  [S, M] float32, out_parent [S, M] int32 (a beam of the same sequence), out_token [S, M] int32, out_finished [S, M] uint8 or NULL (1: the
  *             token is eos, so the beam has ended).  Beyond the last continuation: -inf, -1, -1, 0; such a beam is one that is not in use.
- * status      [S] int32: GR_ROW_OK, or GR_ROW_BAD for a NaN or +inf logit (or finite ones beyond 1e37) of a row that is read, a NaN or +inf score, a temperature that is
+ * status      [S] int32: GR_ROW_OK, or GR_ROW_BAD for a NaN, or a logit above 1e37, in a row that is read, a NaN or +inf score, a temperature that is
  *             not positive and finite: the sequence's outputs are then -inf, -1, -1, 0.
  * The outputs must not overlap the inputs.  Overwrites the handle's selection scratch, as gr_draft does; neither allocates nor synchronises; the same from run to run.
  */

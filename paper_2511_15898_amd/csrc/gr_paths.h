@@ -113,6 +113,7 @@ template <> struct Packed<_Float16> {
 };
 constexpr float kNone = -__builtin_inff();
 constexpr float kMostFloat = 3.402823466e38f;
+constexpr float kMostLogit = 1e37f;                       // a logit above it is a bad entry: so many of a thread's add up below infinity
 
 // From here on the chunk's entries are unpacked again: one instruction each, where keeping them would cost a register each.
 __device__ __forceinline__ void unpack_again(uint4& r) { asm volatile("" : "+v"(r.x), "+v"(r.y), "+v"(r.z), "+v"(r.w)); }

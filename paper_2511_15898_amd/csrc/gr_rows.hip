@@ -229,7 +229,7 @@ __device__ __forceinline__ Scanned scan_slice(ScanLds<EXP, NT>& L, const Rows<T>
         for (int l = 0; l < kLoads; ++l) now[l] = next[l];
         fetch(c0 + kTileChunks);
         const int loads = min(kLoads, (c_end - c0 + NT - 1) / NT);     // of the last tile maybe fewer
-        // Bad: NaN, +inf (logits), negative entries (probabilities).
+        // Bad: NaN, logits above kMostLogit, negative entries (probabilities).
         float top[kLoads], most = kNone, probe = 0.f;
 #pragma unroll
         for (int l = 0; l < kLoads; ++l) {
@@ -247,9 +247,9 @@ __device__ __forceinline__ Scanned scan_slice(ScanLds<EXP, NT>& L, const Rows<T>
             most = fmaxf(most, top[l]);
             unpack_again(now[l]);
         }
-        if (!PROBS && !kExp) bad |= static_cast<int>(!(probe < 3.0e38f));
+        if (!PROBS && !kExp) bad |= static_cast<int>(probe != probe) | static_cast<int>(most > kMostLogit);          // NaN makes the sum NaN
         if (kExp) {
-            bad |= static_cast<int>(most > 3.0e38f);
+            bad |= static_cast<int>(most > kMostLogit);
             es.raise(most, tab);
             if (es.ref == kNone) {
                 // nothing but masked entries and NaN, which the maximum passes over
@@ -432,7 +432,7 @@ __device__ __forceinline__ PieceMass piece_mass(const RowChunks<T, PROBS>& x, in
     }
     float ref = 0.f;
     if (!PROBS) {
-        bad |= static_cast<int>(top > 3.0e38f);
+        bad |= static_cast<int>(top > kMostLogit);
         ref = wave_max_f(top);
         if (ref > kNone && scale > 0.0) {
             ExpSum<true> es(scale);                       // the draws' borders stand on these sums

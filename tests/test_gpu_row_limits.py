@@ -186,3 +186,30 @@ def test_scores_of_zero_tie_whatever_their_sign(torch, gr):
     best, parent, token, over, status = select(torch, gr, x, scores, M, finished=finished, eos=eos)
     assert status.tolist() == [0] * 4 and (parent == [[0, 1, 2, -1, -1]] * 4).all() and (best[:, :3] == 0).all()
     assert (token[:, :3] == np.where(finished, eos, 9)).all() and (over[:, :3] == finished).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("V, rows", [(50, 6), (9001, 6), (70001, 6), (9001, 600)])
+def test_logits_up_to_1e37_and_no_further(torch, gr, dtype, V, rows):
+    """One border for drafts of every kind and for beams: entries up to it are as good as others, however many, one above it makes the row bad; the lowest value never does."""
+    t = getattr(torch, dtype)
+    lowest = float(torch.finfo(t).min)
+    x = torch.zeros((rows, V), dtype=t, device="cuda")
+    x[0] = 9.5e36
+    x[1, V - 2] = 1.1e37
+    x[2, 0] = 1.0e38
+    x[3, 1::2] = 9.9e36; x[3, ::2] = lowest
+    x[4] = lowest; x[4, 3] = 2.0e38
+    bad = np.zeros(rows, bool)
+    bad[[1, 2, 4]] = True
+    u, T = _uniforms(V, rows, 2), np.ones(rows, np.float32)
+    plain = x.float().cpu().numpy()
+    for k in (8, 0):
+        drafts, status = _drafts(torch, gr, x, k, u, T)
+        assert (status == np.where(bad, ROW_BAD, ROW_OK)).all() and (drafts[bad] == -1).all(), k
+        _check_drafts(drafts, plain, k, u, T, some=[0, 3, 5])
+    scores = np.full((rows, 1), -1.0, np.float32)
+    got = select(torch, gr, x[:, None], scores, 4)
+    assert (got[4] == np.where(bad, ROW_BAD, ROW_OK)).all() and (got[1][bad] == -1).all()
+    good = [0, 3, 5]
+    check_beams([v[good] for v in got], plain[good, None], scores[good], 4)
