@@ -122,13 +122,13 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(const Rows<fl
             if (lane < splits) L.lists[b * splits + lane] = n[u];
             const double top = static_cast<double>(wave_max_f(ref[u]));
             const double total = wave_sum(ref[u] > kNone ? sum[u] * exp((static_cast<double>(ref[u]) - top) * inv_temp) : 0.0);
-            bad_beam = bad_beam || __any(bad[u] != 0) || !(score[u] < 3.0e38f);
+            bad_beam = bad_beam || __any(bad[u] != 0) || !(score[u] <= kMostFloat);
             if (lane == 0) { L.top[b] = top; L.log_sum[b] = log(total); L.score[b] = static_cast<double>(score[u]); }
         }
     }
     if (tid == 0) { L.count = 0; L.bad = 0; }
     __syncthreads();
-    if (lane == 0 && (bad_beam || !(temp > 0.f) || !(temp <= 3.0e38f))) L.bad = 1;       // any wave that sets it
+    if (lane == 0 && (bad_beam || !good_temperature(temp))) L.bad = 1;       // any wave that sets it
     __syncthreads();
     const size_t at0 = static_cast<size_t>(seq) * M;
     if (L.bad) {

@@ -34,7 +34,7 @@ __global__ __launch_bounds__(kDraftThreads) void draft_topk_kernel(const float* 
     bool bad = found.bad != 0 || found.total == 0;
     double inv_temp = 1.0;
     if (PROBS) bad = bad || !(fabs(found.qtot - 1.0) <= 1e-3);
-    else if (!(t > 0.f) || !(t <= 3.0e38f)) bad = true;
+    else if (!good_temperature(t)) bad = true;
     else inv_temp = 1.0 / static_cast<double>(t);
     if (bad) {                                            // the same for all threads
         if (tid < out.n) out.drafts[static_cast<size_t>(row) * out.n + tid] = -1;

@@ -113,6 +113,7 @@ template <> struct Packed<_Float16> {
 };
 constexpr float kNone = -__builtin_inff();
 constexpr float kMostFloat = 3.402823466e38f;
+__device__ __forceinline__ bool good_temperature(float t) { return t > 0.f && t <= kMostFloat; }        // NaN: no
 constexpr float kMostLogit = 1e37f;                       // a logit above it is a bad entry: so many of a thread's add up below infinity
 
 // From here on the chunk's entries are unpacked again: one instruction each, where keeping them would cost a register each.

@@ -157,7 +157,7 @@ __device__ __forceinline__ Scanned scan_slice(ScanLds<EXP, NT>& L, const Rows<T>
     double scale = 1.0;
     if (kExp) {
         const float temp = in.temperature_of(row);
-        if (!(temp > 0.f) || !(temp <= 3.0e38f)) bad = 1; else scale = kPerTemp / static_cast<double>(temp);
+        if (!good_temperature(temp)) bad = 1; else scale = kPerTemp / static_cast<double>(temp);
         if (tid < kExpEntries) fill_exp_table(tab);
     }
     if (tid == 0) count = 0;
@@ -390,7 +390,7 @@ __global__ __launch_bounds__(NT) void draft_rows_kernel(const Rows<T> in, int k,
     if (PROBS) q_total = wave_sum(lane < NT / 64 ? q_wave[lane] : 0.0);
     bool bad = mine.found == 0 || any_bad != 0;
     if (PROBS) bad = bad || !(fabs(q_total - 1.0) <= 1e-3);
-    else if (!(t > 0.f) || !(t <= 3.0e38f)) bad = true;
+    else if (!good_temperature(t)) bad = true;
     else inv_temp = 1.0 / static_cast<double>(t);
     if (bad) {                                            // the same for all threads
         if (tid < out.n) out.drafts[static_cast<size_t>(row) * out.n + tid] = -1;
@@ -459,7 +459,7 @@ __device__ __forceinline__ PieceMass piece_mass(const RowChunks<T, PROBS>& x, in
 template <typename T>
 __device__ __forceinline__ double scale_of(const Rows<T>& in, int row) {
     const float temp = in.temperature_of(row);
-    return (temp > 0.f) && (temp <= 3.0e38f) ? kPerTemp / static_cast<double>(temp) : 0.0;
+    return good_temperature(temp) ? kPerTemp / static_cast<double>(temp) : 0.0;
 }
 
 // The sums of a row by pieces, a wave to a piece.  grid = (pieces / 4 * rows).  Bound: HBM (probabilities) or the exponentials; 203 rows of 50021 probabilities 8.8 us (4.6 TB/s).

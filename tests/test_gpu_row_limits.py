@@ -213,3 +213,29 @@ def test_logits_up_to_1e37_and_no_further(torch, gr, dtype, V, rows):
     assert (got[4] == np.where(bad, ROW_BAD, ROW_OK)).all() and (got[1][bad] == -1).all()
     good = [0, 3, 5]
     check_beams([v[good] for v in got], plain[good, None], scores[good], 4)
+
+
+def test_scores_and_temperatures_up_to_the_largest_float(torch, gr):
+    """Positive and finite is all that is asked of a temperature, finite or -inf of a score."""
+    big = float(np.finfo(np.float32).max)
+    S, K, V, M = 4, 2, 3001, 6
+    x = torch.randn((S, K, V), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    rows = x.cpu().numpy()
+    scores = np.array([[big, -1.0], [-big, 3.2e38], [-1.0, -2.0], [-1.0, -2.0]], np.float32)
+    T = np.array([1.0, 1.0, big, 3.2e38], np.float32)
+    finished = np.zeros((S, K), np.uint8)
+    finished[0, 0] = finished[1, 0] = 1
+    check_beams(select(torch, gr, x, scores, M, T, finished=finished, eos=5), rows, scores, M, T, finished=finished, eos=5)
+    u, per_row = _uniforms(3, S * K, 4), np.repeat(T, K)
+    for B in (S * K, 600):
+        y, v, t = x.view(S * K, V).repeat(B // (S * K), 1), np.tile(u, (B // (S * K), 1)), np.tile(per_row, B // (S * K))
+        for k in (0, 30):
+            drafts, status = _drafts(torch, gr, y, k, v, t)
+            assert (status == ROW_OK).all()
+            _check_drafts(drafts, y.cpu().numpy(), k, v, t, some=range(S * K))
+    long = torch.randn((2, 200003), device="cuda", generator=torch.Generator(device="cuda").manual_seed(2))
+    u = _uniforms(4, 2, 4)
+    for k in (0, 30):
+        drafts, status = _drafts(torch, gr, long, k, u, T[2:])
+        assert (status == ROW_OK).all()
+        _check_drafts(drafts, long.cpu().numpy(), k, u, T[2:])
