@@ -288,7 +288,8 @@ typedef struct {
  * first, length  [S] int32 or NULL (0, all tokens); cut to 0..tokens.  Nothing outside is read or written.
  * table       [S K, width] int32 or NULL.  A page that a beam shares with its parent is left as it is; a page that two beams share must not be one that
  *             either gets from a third (pages of a common prompt lie below `first`).  Entries outside 0..blocks-1 are skipped.
- * 1 <= K <= GR_MAX_BEAMS, S <= 65535; strides not below 0, at any alignment; the bytes of different tokens must not overlap.
+ * 1 <= K <= GR_MAX_BEAMS, S <= 65535; strides not below 0, at any alignment; the bytes of different tokens must not overlap.  A block of a pool holds up to
+ * 2 GiB a head, a table's row 2^24 - 1 entries, a dense row as many stretches of 8 KB (or tokens above 8 KB); tokens that lie apart count as 16 bytes at least, and no more than 16 GiB a block.
  * No handle, no scratch; neither allocates nor synchronises.
  */
 int gr_beam_reorder(void* state, const gr_state_layout* layout, const int* parent, const int* first, const int* length, const int* table,

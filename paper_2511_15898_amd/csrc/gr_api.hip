@@ -576,7 +576,7 @@ extern "C" int gr_beam_reorder(void* state, const gr_state_layout* layout, const
     rp.token_stride = a.token_stride; rp.token_bytes = a.token_bytes; rp.row_stride = a.row_stride;
     rp.S = S; rp.K = K; rp.parent = parent; rp.first = first; rp.length = length;
     if (table) {
-        if (a.block < 1 || a.width < 1 || a.blocks < 1 || static_cast<long long>(a.block) * a.width > kMost || a.block * a.token_bytes > kMost) return GR_EINVAL;
+        if (a.block < 1 || a.width < 1 || a.blocks < 1 || static_cast<long long>(a.block) * a.width > kMost || a.token_bytes > kMost / a.block) return GR_EINVAL;
         rp.table = table; rp.width = a.width; rp.blocks = a.blocks; rp.block = a.block;
         rp.tokens = static_cast<long long>(a.block) * a.width;
     } else {
@@ -584,7 +584,7 @@ extern "C" int gr_beam_reorder(void* state, const gr_state_layout* layout, const
         rp.tokens = a.tokens;
     }
     if (K == 1) return GR_OK;                             // a beam alone is its own parent
-    launch_reorder(rp, static_cast<hipStream_t>(hip_stream));
+    if (!launch_reorder(rp, static_cast<hipStream_t>(hip_stream))) return GR_EINVAL;
     return hipGetLastError() != hipSuccess ? GR_EHIP : GR_OK;
 }
 

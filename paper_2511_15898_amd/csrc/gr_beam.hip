@@ -363,35 +363,43 @@ void launch_beam_merge(const RowSource& src, int S, int K, int M, int eos, RowSl
     else run(std::integral_constant<int, 16>{});
 }
 
-void launch_reorder(const ReorderParams& params, hipStream_t stream) {
+bool launch_reorder(const ReorderParams& params, hipStream_t stream) {
+    // what a grid takes along x with 256 threads, and what the kernel counts in 32 bits: units of a chunk, steps of a workgroup
+    constexpr long long kMostChunks = (1 << 24) - 1, kMostUnits = 1 << 30;
     ReorderParams rp = params;
     // heads that lie side by side in a token are part of it
-    if (rp.heads > 1 && rp.head_stride == rp.token_bytes && rp.token_stride == rp.heads * rp.token_bytes) { rp.token_bytes = rp.token_stride; rp.heads = 1; rp.head_stride = 0; }
+    if (rp.heads > 1 && rp.head_stride == rp.token_bytes && rp.token_stride % rp.heads == 0 && rp.token_stride / rp.heads == rp.token_bytes) { rp.token_bytes = rp.token_stride; rp.heads = 1; rp.head_stride = 0; }
     const long long slices = rp.outer * rp.heads;
     if (rp.tokens == 1) rp.token_stride = rp.token_bytes;
     rp.scale = 1;
     if (!rp.table && rp.token_stride == rp.token_bytes) {
         // a dense row whose tokens lie one after the other is so many bytes
         rp.scale = rp.token_bytes;
-        rp.tokens *= rp.scale;
+        if (__builtin_mul_overflow(rp.tokens, rp.scale, &rp.tokens)) return false;
         rp.token_bytes = rp.token_stride = 1;
     }
     // a chunk of a dense row: 8 KB (of 16 rows of 4 MB: 236 us, with 4, 16 and 32 KB 244, 241 and 258)
     if (!rp.table) rp.block = static_cast<int>(std::min(std::max(1ll, 8192 / rp.token_bytes), rp.tokens));
-    const int chunks = static_cast<int>((rp.tokens + rp.block - 1) / rp.block);
+    const long long chunks = (rp.tokens - 1) / rp.block + 1, segments = rp.token_stride == rp.token_bytes ? 1 : rp.block;      // segments: of a chunk, tokens that lie apart
+    long long bytes, chunk_units;
+    if (chunks > kMostChunks || __builtin_mul_overflow(rp.token_bytes, rp.block / segments, &bytes) || __builtin_mul_overflow((bytes - 1) / 16 + 1, segments, &chunk_units) ||
+        chunk_units > kMostUnits)
+        return false;
     // Slices to a workgroup, whose moves and table entries are looked up once: as many as fill the steps in flight (pages of 4 KB: 96 us with 4 slices, 101 with 8, 107 with 16), and the
     // chip wants some thousands of workgroups.
     const long long units = (static_cast<long long>(rp.block) * rp.token_bytes + 16 * kThreads - 1) / (16 * kThreads);
     long long per_group = std::max(1ll, 4 / units);
-    per_group = std::min(per_group, std::max(1ll, slices * chunks * rp.S / 4096));
+    per_group = std::min(per_group, std::max(1ll, std::min(slices, 65536ll) * chunks * rp.S / 4096));
     per_group = std::max(per_group, (slices + 65534) / 65535);
-    const dim3 grid(chunks, rp.S, static_cast<unsigned>((slices + per_group - 1) / per_group));
+    if (per_group * ((chunk_units - 1) / kThreads + 1) > kMostUnits) return false;
+    const dim3 grid(static_cast<unsigned>(chunks), rp.S, static_cast<unsigned>((slices + per_group - 1) / per_group));
     const int pg = static_cast<int>(per_group);
     if (rp.K <= 4) hipLaunchKernelGGL((reorder_kernel<4, 4>), grid, dim3(kThreads), 0, stream, rp, pg);
     else if (rp.K <= 8) hipLaunchKernelGGL((reorder_kernel<8, 2>), grid, dim3(kThreads), 0, stream, rp, pg);
     else if (rp.K <= 16) hipLaunchKernelGGL((reorder_kernel<16, 1>), grid, dim3(kThreads), 0, stream, rp, pg);
     else if (rp.K <= 32) hipLaunchKernelGGL((reorder_kernel<32, 1>), grid, dim3(kThreads), 0, stream, rp, pg);
     else hipLaunchKernelGGL((reorder_kernel<64, 1>), grid, dim3(kThreads), 0, stream, rp, pg);
+    return true;
 }
 
 }  // namespace gr

@@ -68,7 +68,7 @@ struct ReorderParams {
     const int* parent; const int* first; const int* length;
     const int* table; int width; int blocks;
 };
-void launch_reorder(const ReorderParams& rp, hipStream_t stream);
+bool launch_reorder(const ReorderParams& rp, hipStream_t stream);       // false: the kernel's counters do not hold such a row; nothing was launched
 
 // Pages.
 struct PageParams {
