@@ -309,6 +309,7 @@ int gr_beam_reorder(void* state, const gr_state_layout* layout, const int* paren
  * slots       [slots_capacity] int64: for every new token, in order, table entry * block + place in the block (-1 where the entry is below 0); entries from
  *             starts[R] on are left as they are.
  * status      [R] int32.
+ * A released entry goes back as it is, one below 0 too: places below a request's length must hold blocks where they may be released.
  * Blocks are not counted: one that two requests share (a common prompt) must be given back by one of them at most, and not while the other needs it.
  * lengths, new_lengths and free_count are only read, and the out arrays must be others: a decoding loop keeps two sets and swaps them.
  * 1 <= R <= GR_MAX_REQUESTS, R * width, pool and slots_capacity below 2^31.  No handle, no scratch; one launch; neither allocates nor synchronises.

@@ -4,8 +4,8 @@
 //
 // Bound: HBM, one read of the row, where only the largest are asked for (about 5 instructions per element).  With the exponentials, in float64, it is about 20, 12 of them in the
 // innermost loop, and a rate of one instruction for 40 million million elements a second, which float64 has here as float32 has unpacked: 16.5 us for the 29.5 million bfloat16 logits
-// of 230 rows of 128256 that are read in 2.
-// Measured: those 27.5 us; 640 rows of 128256 in float32 81 us (4.0 TB/s); one row of 32000 7.7 us; without sums 256 rows of 128256 in bfloat16, k = 128, 20.6 us (3.2 TB/s).
+// of 230 rows of 128256, whose 59 MB a copy's rate reads in 12.
+// Measured: those 28 us; 640 rows of 128256 in float32 82 us (4.0 TB/s); one row of 32000 8.0 us; without sums 256 rows of 128256 in bfloat16, k = 128, 20.6 us (3.2 TB/s).
 #include <algorithm>
 
 #include "gr_draft.h"
@@ -366,7 +366,8 @@ __global__ __launch_bounds__(kThreads, SUM && !PROBS ? 4 : 5) void rows_kernel(c
 
 // The drafts of rows that one workgroup each reads: grid = (rows), NT threads.  No slices to join, so one launch does, and the candidates never leave LDS.
 // Bound: for one row a chain of dependent steps, 9.5 us for 32000 float32 logits, k = 64, of them 1.5 until the first tile has come, 2.2 for its threshold, 1.0 for the second tile, 1.6
-// to take the list apart, 0.8 to put 118 candidates in order, 0.6 to put 64 in order by id, 0.4 for the draws.  For 256 rows of 128256 in bfloat16 22.5 us, of which the read takes 10.
+// to take the list apart, 0.8 to put 118 candidates in order, 0.6 to put 64 in order by id, 0.4 for the draws.  For 256 rows of 128256 in bfloat16 22.8 us, of which
+// the read takes 10 where the last cache holds the 66 MB (13 at a copy's rate).
 // What all waves repeat costs four times its instructions on a SIMD with four of them, so it is kept short.
 template <typename T, bool PROBS, int NT>
 __global__ __launch_bounds__(NT) void draft_rows_kernel(const Rows<T> in, int k, double tail_mass, const DraftOut out) {
@@ -401,7 +402,8 @@ __global__ __launch_bounds__(NT) void draft_rows_kernel(const Rows<T> in, int k,
 }
 
 // The sum of piece `piece` of a row, a wave's 64 * kLoads chunks one after the other; all lanes hold it.  PROBS: of the entries; logits: of exp((x - ref) / T) with the piece's
-// largest entry as ref, scale 0 for a bad temperature.  A bad entry makes it NaN, and with it the row's total.
+// largest entry as ref, scale 0 for a bad temperature.  A bad entry makes it NaN, and with it the row's total.  The exponentials are the finer ones: 256 rows of 128256 in bfloat16 take 32.2 us
+// where the others took 31.4, 256 of 151936 in float32 35.6 for 33.9.
 struct PieceMass { double mass; float ref; };
 template <typename T, bool PROBS>
 __device__ __forceinline__ PieceMass piece_mass(const RowChunks<T, PROBS>& x, int piece, double scale, const double* tab) {
@@ -478,7 +480,7 @@ __global__ __launch_bounds__(kThreads) void masses_kernel(const Rows<T> in, int 
 }
 
 // Sums and draws of rows that one workgroup each reads, in one launch; the sums by pieces stay in LDS.  grid = (rows), NT threads.
-// Bound: HBM.  203 rows of 50021 probabilities, 16 draws each: 12.4 us (3.3 TB/s), 10.5 where the rows lie in the last cache.
+// Bound: HBM.  203 rows of 50021 probabilities, 16 draws each: 12.0 us (3.4 TB/s), 10.4 where the rows lie in the last cache.
 template <typename T, bool PROBS, int NT>
 __global__ __launch_bounds__(NT) void draft_whole_rows_kernel(const Rows<T> in, int pieces, const DraftOut out) {
     __shared__ double tab[PROBS ? 1 : kExpEntries], mass[kLdsPieces];
@@ -555,10 +557,10 @@ bool draft_in_one(int rows, int V, int dtype) {
     return rows >= kComputeUnits / 2 || static_cast<long long>(V) <= 3ll * 1024 * kLoads * chunk_elements(dtype);
 }
 
-// The same for draws from whole rows.  Short: 32768 logits (their exponentials take longer than the read) or 65536 probabilities.  Measured, two launches against one: a row of 16384 logits
-// in float32 10.7, 8.3, of 32768 10.7, 10.5, of 50021 11.2, 12.9, of 65536 in bfloat16 13.1, 15.7; of 65536 probabilities 9.9, 8.3, of 98304 10.0, 10.7.  192 rows and more: 203 of
-// 50021 probabilities, 16 draws each, 14.5, 10.7; 203 of 128256 in bfloat16 34.7, 36.3, 256 of them 38.6, 37.2; 256 of 151936 in float32 43.7, 37.3.  More rows than compute units: with
-// 512 threads 1024 rows of 16384 in float32 take 22.4, with 1024 threads 25.6, in two launches 26.3; 4096 of 2048 44.4, 56.3, 41.0.
+// The same for draws from whole rows.  Short: 32768 logits (their exponentials take longer than the read) or 65536 probabilities.  Measured, two launches against one, 4 draws a row, us per call: a row of
+// 16384 logits in float32 9.8, 8.4, of 32768 10.0, 10.6, of 50021 10.8, 13.5, of 65536 in bfloat16 12.6, 16.1; of 65536 probabilities 9.4, 7.0, of 98304 9.3, 8.8.  192 rows and more: 203 of
+// 50021 probabilities, 16 draws each, 13.8, 11.4; 203 of 128256 in bfloat16 28.9, 29.7, 256 of them 32.5, 30.2; 256 of 151936 in float32 41.9, 36.6.  More rows than compute units: with
+// 512 threads 1024 rows of 16384 in float32 take 25.8, with 1024 threads 26.8, in two launches 26.5; 4096 of 2048 47.2, 55.5, 42.4.
 bool draft_whole_in_one(int rows, int V, int dtype, bool probs) {
     return piece_count(V, dtype) <= kLdsPieces && (4 * rows >= 3 * kComputeUnits || V <= (probs ? 65536 : 32768));
 }
